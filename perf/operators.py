@@ -182,7 +182,7 @@ def prepare(case, seed):
         s["g"] = torch.nn.functional.logsigmoid(normal(rows, H) + 3.0)
         if own:                                # the work memory that a sampling program keeps
             import paper_2608_28158_b200 as hp
-            s["workspace"] = torch.empty(hp.harts_gen_la_workspace_bytes(n, s["max_len"], H, d, d, dt), dtype=torch.uint8, device="cuda")
+            s["workspace"] = torch.empty(hp.harts_gen_la_workspace_bytes(n, s["max_len"], rows, H, d, d, dt), dtype=torch.uint8, device="cuda")
         return s
     if case["op"] in ("write", "read"):
         n, hk, page, pages = case["tokens"], case["kv_heads"], case["page"], case["pages"]
