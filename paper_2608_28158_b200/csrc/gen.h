@@ -1,0 +1,59 @@
+// Internal launch interface of the sampling calls between the C ABI (gen_api.cu) and the kernel files.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/harts_gen.h"
+
+namespace harts {
+
+struct GenLaArgs {
+    int32_t n_seq;
+    const int32_t *seq_begin, *seq_len, *in_state, *out_state;
+    int32_t max_len;
+    int64_t n_rows;
+    const void *q, *k, *v;
+    int64_t ld_q, ld_k, ld_v;
+    const float* g;
+    void* o;
+    float* states;
+    int32_t n_states, H, d, dtype;
+    void* workspace;
+    int32_t* dev_status;
+    cudaStream_t stream;
+};
+
+int32_t gen_la_walk(const GenLaArgs& a);          // gen_la_walk.cu: token by token, state in registers
+
+// Chunked form (bf16, d = 128): a sequence is one item, or several segments of whole chunks that one item each walks.
+struct GenItems {
+    const int32_t* count;     // device: items there are
+    const int4* items;        // device: first row, rows, start state (>= 0: in the pool, -1: zero, -2 - i: starts[i]), last state's place or -1
+    float* starts;            // [item, H, 128, 128] start states of segments
+};
+int32_t gen_la_chunks(const GenLaArgs& a);        // gen_la_chunk.cu
+bool gen_la_chunked(const GenLaArgs& a);
+size_t gen_la_chunk_bytes(const GenLaArgs& a);    // workspace of gen_la_chunks
+int32_t pipe_gen(const GenLaArgs& a, const GenItems& items, int64_t max_items);      // la_pipe_fwd.cu
+
+#ifdef __CUDACC__
+// a sequence's entries, checked: false where one is out of range (one thread of the caller reports it)
+struct GenSeq {
+    int begin, len, in, out;
+};
+__device__ __forceinline__ bool gen_seq(const GenLaArgs& a, int i, GenSeq& s) {
+    s.begin = a.seq_begin[i];
+    s.len = a.seq_len[i];
+    s.in = a.in_state[i];
+    s.out = a.out_state[i];
+    return s.begin >= 0 && s.len >= 0 && s.len <= a.max_len && (int64_t)s.begin + s.len <= a.n_rows && s.in >= -1 && s.in < a.n_states &&
+           s.out >= -1 && s.out < a.n_states;
+}
+__device__ __forceinline__ void gen_report(int32_t* status, int position) {
+    if (status && atomicCAS(status, 0, HARTS_EINVAL) == 0) status[1] = position;
+}
+#endif
+
+}  // namespace harts

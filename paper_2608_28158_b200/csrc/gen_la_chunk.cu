@@ -1,0 +1,330 @@
+// Linear attention from and into kept states in chunks (bf16, d = 128): the work table, and what lets several CTAs share one long
+// sequence.
+//
+// The walk itself is pipe_fwd_kernel (la_pipe_fwd.cu): 1.5 us a chunk and head where the chain of chunks is what counts.  A sequence that
+// is long beside what every SM has to do is cut into segments of L chunks, whose start states are found first:
+//     U_i = sum over segment i of e^{B_end - B_j} k_j^T v_j,   S_{i+1} = e^{B_i} S_i + U_i
+// The sums do not depend on each other (one product of k~^T v with the tokens as its inner dimension, left in tensor memory until the
+// segment's end); the recurrence over segments is a multiply-add per element.  That reads k and v twice, and 192 KB a segment and head.
+#include "gen.h"
+#include "kernels.h"
+#include "tc_common.cuh"
+
+namespace harts {
+
+int32_t make_row_map_ld(CUtensorMap* map, const void* base, int64_t rows, int32_t H, int64_t ld);
+int sm_count();
+
+namespace {
+
+using namespace tc;
+
+constexpr int BT = 64, D = 128;
+constexpr int MAX_L = 48;                     // chunks of a segment (its weights stay in shared memory)
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Sizes {
+    int64_t max_items;
+    int L;                                    // chunks of a segment, 0: sequences are not cut
+    size_t items, follows, chains, gamma, starts, total;
+};
+Sizes sizes_of(const GenLaArgs& a) {
+    Sizes z;
+    const int64_t longest = ((int64_t)a.max_len + BT - 1) / BT;
+    int64_t chunks = a.n_rows / BT + a.n_seq;                       // there are at most that many
+    if (chunks > longest * a.n_seq) chunks = longest * a.n_seq;
+    const int64_t share = (chunks * a.H + sm_count() - 1) / sm_count(), room = sm_count() / a.H - a.n_seq;
+    z.L = 0;
+    if (longest > 8 && 2 * longest > 3 * share) {
+        const int64_t L = room > 0 ? (chunks + room - 1) / room : (share + 1) / 2;
+        z.L = (int)(L < 4 ? 4 : L > MAX_L ? MAX_L : (L + 3) / 4 * 4);
+    }
+    z.max_items = a.n_seq + (z.L ? chunks / z.L : 0);
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    z.items = 256;
+    z.follows = up(z.items + (size_t)z.max_items * sizeof(int4));
+    z.chains = up(z.follows + (size_t)z.max_items * sizeof(int));
+    z.gamma = up(z.chains + (size_t)a.n_seq * sizeof(int4));
+    z.starts = up(z.gamma + (z.L ? (size_t)z.max_items * a.H * sizeof(float) : 0));
+    z.total = z.starts + (z.L ? (size_t)z.max_items * a.H * D * D * sizeof(float) : 0);
+    return z;
+}
+
+constexpr int PLAN_THREADS = 512;
+// Items in the order of the sequences, and each sequence's {first item, items, start state, -}.
+__global__ void __launch_bounds__(PLAN_THREADS)
+plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, int* follows, int4* chains) {
+    __shared__ int warp_sum[PLAN_THREADS / 32], base;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) base = 0;
+    __syncthreads();
+    const int rows = L ? L * BT : INT32_MAX;
+    for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) {
+        const int i = i0 + tid;
+        GenSeq s;
+        int n = 0;
+        if (i < a.n_seq) {
+            if (!gen_seq(a, i, s)) gen_report(a.dev_status, i);
+            else if (s.out >= 0 || (a.o && s.len > 0)) n = s.len == 0 ? 1 : (s.len - 1) / rows + 1;
+        }
+        int upto = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 31) warp_sum[warp] = upto;
+        __syncthreads();
+        int ahead = base;
+        for (int w = 0; w < warp; w++) ahead += warp_sum[w];
+        upto += ahead;
+        if (n > 0 && upto > max_items) {               // rows that sequences share: more items than the rows allow
+            gen_report(a.dev_status, i);
+            n = 0;
+        } else if (n > 0) {
+            const int first = upto - n;
+            for (int j = 0; j < n; j++) {
+                items[first + j] = make_int4(s.begin + j * rows, j + 1 < n ? rows : s.len - j * rows, n > 1 ? -2 - (first + j) : s.in, j + 1 < n ? -1 : s.out);
+                follows[first + j] = j + 1 < n;
+            }
+            chains[i] = make_int4(first, n, s.in, 0);
+        }
+        if (n == 0 && i < a.n_seq) chains[i] = make_int4(0, 0, -1, 0);
+        __syncthreads();
+        if (tid == PLAN_THREADS - 1) base = min(upto, max_items);
+        __syncthreads();
+    }
+    if (tid == 0) *count = base;
+}
+
+// ---- sums of segments --------------------------------------------------------------------------------------------------------
+constexpr int PANEL = BT * 128, TILE = 2 * PANEL, STAGE = 3 * TILE, STAGES = 2, SUM_THREADS = 288, SUM_WARPS = 8;
+struct SumMisc {
+    float w[MAX_L * BT];
+    float warp_sum[SUM_WARPS];
+    uint64_t full[STAGES], ready[STAGES], done[STAGES];
+    uint32_t tmem;
+    int dead;
+};
+constexpr int SUM_BYTES = STAGES * STAGE + sizeof(SumMisc) + 1024;
+
+__global__ void __launch_bounds__(SUM_THREADS, 2)
+sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const float* __restrict__ g, int H,
+           const GenItems gen, const int* __restrict__ follows, float* __restrict__ gamma, int* status) {
+    after_previous();
+    const int item = blockIdx.x / H, h = blockIdx.x % H;
+    if (item >= *gen.count || !follows[item]) return;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    SumMisc& m = *reinterpret_cast<SumMisc*>(smem + STAGES * STAGE);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int4 it = gen.items[item];
+    const int begin = it.x, len = it.y, n_chunks = len / BT;           // whole chunks: only a sequence's last segment may end inside one
+    if (tid == 0) {
+        for (int i = 0; i < STAGES; i++) {
+            mbar_init(&m.full[i], 1);
+            mbar_init(&m.ready[i], SUM_WARPS);
+            mbar_init(&m.done[i], 1);
+        }
+        m.dead = 0;
+        fence_barrier_init();
+    }
+    if (warp == 0) {
+        __syncwarp();
+        tmem_alloc<128>(&m.tmem);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = m.tmem;
+    if (warp == SUM_WARPS) {
+        // ---- loads and products ------------------------------------------------------------------------------------------------
+        auto load = [&](int c) {
+            unsigned char* tile = smem + (c % STAGES) * STAGE;
+            mbar_expect_tx(&m.full[c % STAGES], 2 * TILE);
+            for (int p = 0; p < 2; p++) {
+                tma_load_3d(tile + p * PANEL, &map_k, p * 64, h, begin + c * BT, &m.full[c % STAGES]);
+                tma_load_3d(tile + TILE + p * PANEL, &map_v, p * 64, h, begin + c * BT, &m.full[c % STAGES]);
+            }
+        };
+        if (lane == 0)
+            for (int c = 0; c < STAGES && c < n_chunks; c++) load(c);
+        __syncwarp();
+        constexpr uint32_t IDESC = instr_desc(128, 128, 1, 1);
+        for (int c = 0; c < n_chunks; c++) {
+            const int st = c % STAGES;
+            const uint32_t ph = (c / STAGES) & 1;
+            if (!mbar_wait_warp(&m.ready[st], ph, status, &m.dead)) break;
+            tc_fence_after();
+            const uint32_t tile = smem_u32(smem + st * STAGE);
+            if (elect_one()) {
+#pragma unroll
+                for (int term = 0; term < 2; term++)
+#pragma unroll
+                    for (int ks = 0; ks < 4; ks++)
+                        mma_ss(tmem, desc_mnmajor<BT>(tile + term * 2 * TILE, ks), desc_mnmajor<BT>(tile + TILE, ks), IDESC, c > 0 || term > 0 || ks > 0);
+                mma_commit(&m.done[st]);
+            }
+            __syncwarp();
+            if (c + STAGES < n_chunks) {
+                if (!mbar_wait_warp(&m.done[st], ph, status, &m.dead)) break;
+                if (lane == 0) load(c + STAGES);
+                __syncwarp();
+            }
+        }
+    } else {
+        // ---- weights e^{B_end - B_j}: L / 4 tokens in a row per thread, summed from the end --------------------------------------------
+        for (int e = tid; e < len; e += 256) m.w[e] = g[(size_t)(begin + e) * H + h] * LOG2E;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const int per = len / 256;
+        float own = 0.f;
+        for (int e = 0; e < per; e++) own += m.w[tid * per + e];
+        float behind = own;                       // of this thread and the ones behind it in the warp
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const float y = __shfl_down_sync(~0u, behind, d);
+            if (lane + d < 32) behind += y;
+        }
+        if (lane == 0) m.warp_sum[warp] = behind;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        float after = __shfl_down_sync(~0u, behind, 1), total = 0.f;
+        if (lane == 31) after = 0.f;
+        for (int w = 0; w < SUM_WARPS; w++) {
+            if (w > warp) after += m.warp_sum[w];
+            total += m.warp_sum[w];
+        }
+        for (int e = per - 1; e >= 0; e--) {
+            const float y = m.w[tid * per + e];
+            m.w[tid * per + e] = ex2(after);
+            after += y;
+        }
+        if (tid == 0) gamma[(size_t)item * H + h] = ex2(total);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        for (int c = 0; c < n_chunks; c++) {
+            const int st = c % STAGES;
+            if (!mbar_wait_warp(&m.full[st], (c / STAGES) & 1, status, &m.dead)) break;
+            unsigned char* tile = smem + st * STAGE;
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int e = tid + u * 256, t = (e >> 3) & (BT - 1), off = (e >> 9) * PANEL + sw128_chunk(t, e & 7);
+                const float w = m.w[c * BT + t];
+                uint4 y = *reinterpret_cast<const uint4*>(tile + off), z;
+                auto terms = [&](uint32_t& x, uint32_t& rest) {
+                    const float p0 = __uint_as_float(x << 16) * w, p1 = __uint_as_float(x & 0xffff0000u) * w;
+                    x = pack_bf16(p0, p1);
+                    rest = pack_bf16(p0 - __uint_as_float(x << 16), p1 - __uint_as_float(x & 0xffff0000u));
+                };
+                terms(y.x, z.x);
+                terms(y.y, z.y);
+                terms(y.z, z.z);
+                terms(y.w, z.w);
+                *reinterpret_cast<uint4*>(tile + off) = y;
+                *reinterpret_cast<uint4*>(tile + 2 * TILE + off) = z;
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.ready[st]);
+        }
+        const int last = n_chunks - 1;
+        const bool ok = mbar_wait_warp(&m.done[last % STAGES], (last / STAGES) & 1, status, &m.dead);
+        tc_fence_after();
+        if (ok) {
+            const int quarter = warp & 3, half = warp >> 2;
+            float* dst = gen.starts + ((size_t)item * H + h) * (D * D) + (size_t)(quarter * 32 + lane) * D + half * 64;
+#pragma unroll
+            for (int b = 0; b < 2; b++) {
+                uint32_t x[32];
+                tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + half * 64 + b * 32, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    *reinterpret_cast<uint4*>(dst + b * 32 + 4 * e) = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+            }
+        }
+        tc_fence_before();
+    }
+    __syncwarp();
+    if (__syncthreads_or(m.dead)) drain_delay();          // abandoned: copies and MMAs in flight must land before the CTA goes
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc<128>(tmem);
+}
+
+// ---- start states of segments: starts[i] holds U_i on entry and S_i afterwards; four elements a thread -------------------------------
+constexpr int AHEAD = 8;
+__global__ void __launch_bounds__(256)
+scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const int4* __restrict__ chains, const float* __restrict__ gamma, int H) {
+    after_previous();
+    const int4 chain = chains[blockIdx.z];
+    if (chain.y < 2) return;
+    const int h = blockIdx.y;
+    const size_t off = (size_t)(blockIdx.x * 256 + threadIdx.x) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (chain.z >= 0) s = *reinterpret_cast<const float4*>(states + ((size_t)chain.z * H + h) * (D * D) + off);
+    auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)(chain.x + j) * H + h) * (D * D) + off); };
+    for (int j0 = 0; j0 < chain.y; j0 += AHEAD) {
+        float4 u[AHEAD];
+        float e[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++)
+            if (j0 + j + 1 < chain.y) {
+                u[j] = *at(j0 + j);
+                e[j] = gamma[(size_t)(chain.x + j0 + j) * H + h];
+            }
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++)
+            if (j0 + j < chain.y) {
+                *at(j0 + j) = s;
+                if (j0 + j + 1 < chain.y) {
+                    s.x = fmaf(e[j], s.x, u[j].x);
+                    s.y = fmaf(e[j], s.y, u[j].y);
+                    s.z = fmaf(e[j], s.z, u[j].z);
+                    s.w = fmaf(e[j], s.w, u[j].w);
+                }
+            }
+    }
+}
+
+}  // namespace
+
+// Tokens one by one or chunks: see the figures at the head of gen_la_walk.cu.
+bool gen_la_chunked(const GenLaArgs& a) { return a.dtype == HARTS_BF16 && a.d == 128 && a.max_len > 16; }
+
+size_t gen_la_chunk_bytes(const GenLaArgs& a) { return sizes_of(a).total; }
+
+int32_t gen_la_chunks(const GenLaArgs& a) {
+    const Sizes z = sizes_of(a);
+    char* ws = static_cast<char*>(a.workspace);
+    if (z.max_items * a.H * 2 > INT32_MAX) return HARTS_EINVAL;
+    int* count = reinterpret_cast<int*>(ws);
+    int4 *items = reinterpret_cast<int4*>(ws + z.items), *chains = reinterpret_cast<int4*>(ws + z.chains);
+    int* follows = reinterpret_cast<int*>(ws + z.follows);
+    float *gamma = reinterpret_cast<float*>(ws + z.gamma), *starts = reinterpret_cast<float*>(ws + z.starts);
+    plan_kernel<<<1, PLAN_THREADS, 0, a.stream>>>(a, z.L, (int)z.max_items, count, items, follows, chains);
+    if (cudaGetLastError() != cudaSuccess) return HARTS_ECUDA;
+    const GenItems gen{count, items, starts};
+    if (z.L) {
+        CUtensorMap mk, mv;
+        int32_t rc;
+        if ((rc = make_row_map_ld(&mk, a.k, a.n_rows, a.H, a.ld_k)) != HARTS_OK) return rc;
+        if ((rc = make_row_map_ld(&mv, a.v, a.n_rows, a.H, a.ld_v)) != HARTS_OK) return rc;
+        if (cudaFuncSetAttribute(sum_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SUM_BYTES) != cudaSuccess) return HARTS_ECUDA;
+        if (launch_after(sum_kernel, (int)(z.max_items * a.H), SUM_THREADS, SUM_BYTES, a.stream, mk, mv, a.g, a.H, gen, (const int*)follows, gamma,
+                         a.dev_status) != cudaSuccess)
+            return HARTS_ECUDA;
+        cudaLaunchAttribute ahead{};
+        ahead.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        ahead.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t c{};
+        c.gridDim = dim3(D * D / 1024, (unsigned)a.H, (unsigned)a.n_seq);
+        c.blockDim = dim3(256);
+        c.stream = a.stream;
+        c.attrs = &ahead;
+        c.numAttrs = 1;
+        if (cudaLaunchKernelEx(&c, scan_kernel, (const float*)a.states, starts, (const int4*)chains, (const float*)gamma, (int)a.H) != cudaSuccess)
+            return HARTS_ECUDA;
+    }
+    return pipe_gen(a, gen, z.max_items);
+}
+
+}  // namespace harts

@@ -16,6 +16,11 @@
 // Outputs are staged over the q rows they were made of, and the gate warp, which reuses their chunk's record next, sends them off.
 // Every wait is bounded; one that runs out latches, and the CTA leaves all loops.
 //
+// GEN: the same walk from and into kept states (harts_gen_la): the items come from a table that the call's first kernel has written, there
+// is neither replay nor a chunk-state workspace, and the state behind an item's last chunk is wanted.  It has to be as good as fp32 sums of
+// the given keys and values, so a weighted key is two bf16 terms, the second in a tile of its own, and K~^T V two products.  Rows
+// behind an item's end belong to others and may hold anything: a partial chunk's keys and values are zeroed there.
+//
 // What bounds it: HBM where chains are many (4,696 chunks x 32 heads 2,946 -> 2,480 us, 98 KB an item: 5.9 TB/s; 2,389 x 16 in chains of
 // up to 293 chunks 1,230 -> 700), else the 1.5 us of a chunk's busiest role (1,047 x 16 in 64 chains, two slices each: scan and chunk
 // kernel 492 -> 400).  First figures: the synchronous walk of la_tc_fwd.cu or la_scan.cu with la_chunk_fwd.cu.  What made it:
@@ -25,12 +30,14 @@
 //   * two values an instruction in the element-wise passes, masking without exponentials off the diagonal (2,710 -> 2,640);
 //   * the switch to the next sequence: start state by whole sectors and asked of the L2 when the sequence is drawn, replayed rows with
 //     more copies in flight (2,690 -> 2,480; 249 branchy sequences' worth of 3,439 chunks x 16: 1,383 -> 1,076).
+#include "gen.h"
 #include "kernels.h"
 #include "tc_common.cuh"
 
 namespace harts {
 
 int32_t make_row_map(CUtensorMap* map, const void* base, int64_t rows, int32_t H);
+int32_t make_row_map_ld(CUtensorMap* map, const void* base, int64_t rows, int32_t H, int64_t ld);
 int32_t make_state_map(CUtensorMap* map, const void* base, int64_t n);
 int sm_count();
 
@@ -46,33 +53,35 @@ constexpr int RAW = 8, ITEMS = 4, EXPORTS = 4;                 // rings: raw log
 constexpr int PANEL = BT * 128, S_PANEL = D * 128;
 constexpr float LOG2E = 1.4426950408889634f;
 
-template <int NV>
+template <int NV, bool GEN>
 struct Shape {
     static constexpr int CW = NV / 2;                      // state columns per state thread
-    static constexpr int STAGES = NV == 64 ? 4 : 3;        // chunks of rows in shared memory, and chunk records: as many, since the
+    static constexpr int STAGES = NV == 64 && !GEN ? 4 : 3;        // chunks of rows in shared memory, and chunk records: as many, since the
                                                            // gate warp gives a stage back when it reuses the record
     static constexpr int OUTS = NV == 64 ? 2 : 1;          // state tiles
     static constexpr int OB = NV == 64 ? 2 : 1;            // output accumulators
     static constexpr int VP = NV / 64;                     // panels of 64 columns of v, the state and the outputs
     static constexpr int Q = 0, K = 2 * PANEL, V = 4 * PANEL, STAGE = V + VP * PANEL, S = VP * S_PANEL;
-    static constexpr int s = STAGES * STAGE, p = s + OUTS * S, misc = p + 2 * PANEL, bytes = misc + 9216 + 1024;
+    static constexpr int s = STAGES * STAGE, p = s + OUTS * S, lo = p + 2 * PANEL, misc = lo + (GEN ? 2 * PANEL : 0), bytes = misc + 9216 + 1024;
     // tensor memory: sums of a chunk (two), A (two), outputs (P V and Q S side by side)
     static constexpr int COL_U = 0, COL_A = 2 * NV, COL_O = COL_A + 128, COLS = 512;
     static_assert(COL_O + OB * 128 <= COLS, "tensor memory");
+    static_assert(bytes <= 227 * 1024, "shared memory");
 };
 struct Item {                // one (sequence, head, slice); seq < 0: no more
     int seq, h, slice, own_begin, n_replay, n_virtual, n_chunks, chunk_base, replay_base, init_slot, req_lo, req_hi;
+    int out;                 // GEN: the state that the last one goes to, or -1
 };
 struct Record {              // one chunk
     float nb2[BT];           // minus the running log-decay, in log2 units
     float eb[BT];            // e^{b_t}
     float part[BT];          // rows 0..31: e^{b_31 - b_j}, rows 32..63: e^{b_t - b_31}; their product is the decay between the halves
-    uint2 w[BT];             // e^{b_n - b_t} as the sum of two bf16, each twice
+    uint2 w[BT];             // e^{b_n - b_t} as the sum of two bf16, each twice (GEN: as it is)
     int code[BT];            // physical row of an output (own rows), -1 elsewhere
     float gamma;             // e^{b_n}
     int h, col0, row0;       // row0: physical row of the chunk's first row, where all 64 are own rows (full)
     int full, step, end;     // step: the state is needed behind this chunk; end: no chunk, no more to come
-    int pad;
+    int valid;               // GEN: rows of the chunk that are the item's
 };
 struct Misc {
     Record rows[4];
@@ -135,23 +144,35 @@ __device__ __forceinline__ void mma_lo(uint32_t d, uint32_t a, uint32_t b, uint3
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(DESC_HI), "r"(idesc), "n"(ADD ? 1 : 0) : "memory");
 }
 // d (+)= sum over k-steps; the lower words advance by SA, SB a step, by GA more behind the fourth (K contiguous: the next panel)
-template <int STEPS, int SA, int SB, int GA, int GB>
+template <int STEPS, int SA, int SB, int GA, int GB, bool ADD = false>
 __device__ __forceinline__ void mma_steps(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
-    mma_lo<false>(d, a, b, idesc);
+    mma_lo<ADD>(d, a, b, idesc);
 #pragma unroll
     for (int ks = 1; ks < STEPS; ks++) mma_lo<true>(d, a + ks * SA + (ks >> 2) * GA, b + ks * SB + (ks >> 2) * GB, idesc);
 }
 
-template <int NV>
+// A weighted pair of keys, w k, as two terms of bf16.
+__device__ __forceinline__ void two_terms(uint32_t& x, uint32_t& rest, F2 w) {
+    float a, b;
+    f2_split(f2_mul(f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)), w), a, b);
+    x = pack_bf16(a, b);
+    rest = pack_bf16(a - __uint_as_float(x << 16), b - __uint_as_float(x & 0xffff0000u));
+}
+
+template <int NV, bool GEN>
 __global__ void __launch_bounds__(NT, 1)
-pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, const __grid_constant__ CUtensorMap map_q,
+pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int n_items, int H, const __grid_constant__ CUtensorMap map_q,
                 const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                 const __grid_constant__ CUtensorMap map_cs, const __grid_constant__ CUtensorMap map_o,
                 const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* __restrict__ k, const __nv_bfloat16* __restrict__ v,
                 const float* __restrict__ g, __nv_bfloat16* __restrict__ o, float* slots, int store_states, int* status,
                 const int32_t* gate, int* flags, int* ticket) {
     if (gate_closed(gate)) return;
-    using S = Shape<NV>;
+    if constexpr (GEN) {                          // the items are the previous kernel's, and so may the start states be
+        after_previous();
+        n_items = *gen.count * H * (D / NV);
+    }
+    using S = Shape<NV, GEN>;
     constexpr int SLICES = D / NV, CW = S::CW, STAGES = S::STAGES, OUTS = S::OUTS, OB = S::OB, VP = S::VP;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -192,6 +213,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = m.tmem;
+    auto state_of = [&](int at, int h) {          // GEN: a state of the pool, or the start of an item that continues another one
+        return (at >= 0 ? slots + (size_t)at * H * (D * D) : gen.starts + (size_t)(-2 - at) * H * (D * D)) + (size_t)h * (D * D);
+    };
     // a whole warp; parity: of the phase that has to be over (a barrier just initialised: 1 is over)
     auto wait = [&](uint64_t* bar, uint32_t parity) { return __builtin_expect(__all_sync(~0u, mbar_try(bar, parity)), 1) || wait_on(bar, parity, &m); };
     // two at once, both tries in flight
@@ -213,6 +237,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
         for (; alive && wait(&m.item_full[ri.i], ri.ph);) {
             const Item& item = m.items[ri.i];
             const int seq = item.seq, h = item.h, slice = item.slice, n_chunks = item.n_chunks, init_slot = item.init_slot, req_hi = item.req_hi;
+            const int out = GEN ? item.out : -1;
             int req = item.req_lo;
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.item_empty[ri.i]);
@@ -222,9 +247,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
             F2 x[CW / 2];
 #pragma unroll
             for (int e = 0; e < CW / 2; e++) x[e] = f2(0.f, 0.f);
-            if (init_slot >= 0) {
+            if (GEN ? init_slot != -1 : init_slot >= 0) {
                 const size_t from = (size_t)init_slot * H + h;
-                const float* src = slots + from * (D * D) + in_state;
+                const float* src = (GEN ? state_of(init_slot, h) : slots + from * (D * D)) + in_state;
                 if (ticket) alive = flag_wait_warp(flags + from * SLICES + slice, 1, status, &m.dead);
                 // a thread's row is 512 bytes from the next one's: whole sectors at a time, where the array allows it
                 if ((reinterpret_cast<uintptr_t>(slots) & 31) == 0) {
@@ -269,7 +294,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                     req++;
                     boundary = req < req_hi ? tb.slot_chunk[req] : -1;
                 }
-                const bool step = c + 1 < n_chunks;       // behind the last chunk nobody needs the state
+                const bool step = c + 1 < n_chunks || out >= 0;       // behind the last chunk nobody needs the state, unless it is kept
                 alive = step ? wait_both(&m.gates_full[rg.i], rg.ph, &m.u_full[ru.i], ru.ph) : wait(&m.gates_full[rg.i], rg.ph);
                 if (step) {
                     const float gamma = m.rows[rg.i].gamma;
@@ -290,13 +315,24 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                 if (lane == 0) mbar_arrive(&m.gates_empty[rg.i]);
                 rg.next();
             }
+            if (GEN && out >= 0 && alive) {
+                float4* to = reinterpret_cast<float4*>(state_of(out, h) + in_state);
+#pragma unroll
+                for (int e = 0; e < CW / 4; e++) {
+                    float4 y;
+                    f2_split(x[2 * e], y.x, y.y);
+                    f2_split(x[2 * e + 1], y.z, y.w);
+                    to[e] = y;
+                }
+            }
         }
     } else if (warp < (NS + NW) / 32) {
         // ---- work: masking of A, weighting of k ---------------------------------------------------------------------------------
         const int quarter = warp & 3, t = quarter * 32 + lane;
         const uint32_t tm_lane = tmem + ((uint32_t)(quarter * 32) << 16) + S::COL_A;
         Ring<STAGES> rg;
-        Ring<2> ra;
+        Ring<2> ra, rl;                           // rl: sums, the first of two terms each (GEN)
+        bool summed = false;
         uint32_t seen[16];                        // the diagonal's 32 columns, two to a register: ones where the row sees the column
 #pragma unroll
         for (int e = 0; e < 16; e++) seen[e] = (2 * e <= lane ? 0xffffu : 0u) | (2 * e + 1 <= lane ? 0xffff0000u : 0u);
@@ -354,7 +390,47 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                 fence_async_smem();
             } else {                              // k rows weighted in place, once A has been made of them: a panel of 64 columns per warp
                 if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph)) break;
-                if (rd.step) {
+                if constexpr (GEN) {
+                    const int valid = rd.valid;
+                    if (rd.step) {
+                        // the tile of second terms: the sum before this one has been made
+                        if (summed) {
+                            if (!wait(&m.u_full[rl.i], rl.ph)) break;
+                            rl.next();
+                        }
+                        summed = true;
+                        unsigned char *sk = smem + rg.i * S::STAGE + S::K + (quarter - 2) * PANEL, *sl = smem + S::lo + (quarter - 2) * PANEL;
+#pragma unroll 1
+                        for (int t0 = lane >> 3; t0 < BT; t0 += 16) {
+                            uint4 y[4];
+                            float w[4];
+#pragma unroll
+                            for (int u = 0; u < 4; u++) {
+                                y[u] = *reinterpret_cast<const uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7));
+                                w[u] = __uint_as_float(rd.w[t0 + 4 * u].x);
+                                if (t0 + 4 * u >= valid) y[u] = make_uint4(0, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int u = 0; u < 4; u++) {
+                                uint4 z;
+                                const F2 w2 = f2(w[u], w[u]);
+                                two_terms(y[u].x, z.x, w2);
+                                two_terms(y[u].y, z.y, w2);
+                                two_terms(y[u].z, z.z, w2);
+                                two_terms(y[u].w, z.w, w2);
+                                *reinterpret_cast<uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7)) = y[u];
+                                *reinterpret_cast<uint4*>(sl + sw128_chunk(t0 + 4 * u, lane & 7)) = z;
+                            }
+                        }
+                    }
+                    if (valid < BT && quarter - 2 < VP) {
+                        unsigned char* sv = smem + rg.i * S::STAGE + S::V + (quarter - 2) * PANEL;
+#pragma unroll 1
+                        for (int t = valid + (lane >> 3); t < BT; t += 4)
+                            *reinterpret_cast<uint4*>(sv + sw128_chunk(t, lane & 7)) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                } else if (rd.step) {
                     unsigned char* sk = smem + rg.i * S::STAGE + S::K + (quarter - 2) * PANEL;
 #pragma unroll 1
                     for (int t0 = lane >> 3; t0 < BT; t0 += 16) {
@@ -457,7 +533,19 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
             }
             Item it;
             it.seq = -1;
-            if (pos < n_items) {
+            it.out = -1;
+            if (GEN && pos < n_items) {
+                it.slice = pos % SLICES;
+                it.h = pos / SLICES % H;
+                it.seq = pos / SLICES / H;
+                const int4 e = gen.items[it.seq];
+                it.own_begin = e.x;
+                it.n_replay = it.replay_base = it.req_lo = it.req_hi = it.chunk_base = 0;
+                it.n_virtual = e.y;
+                it.n_chunks = (e.y + BT - 1) / BT;
+                it.init_slot = e.z;
+                it.out = e.w;
+            } else if (!GEN && pos < n_items) {
                 it.slice = pos % SLICES;
                 it.h = pos / SLICES % H;
                 const int sp = seq_lo + pos / SLICES / H;
@@ -483,8 +571,8 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
             }
             ri.next();
             if (it.seq < 0) break;
-            if (lane == 0 && it.init_slot >= 0 && it.slice == 0)      // its start state into the L2, chunks ahead of its use
-                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(slots + ((size_t)it.init_slot * H + it.h) * (D * D)), "n"(D * D * 4) : "memory");
+            if (lane == 0 && (GEN ? it.init_slot != -1 : it.init_slot >= 0) && it.slice == 0)      // its start state into the L2, chunks ahead of its use
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(GEN ? state_of(it.init_slot, it.h) : slots + ((size_t)it.init_slot * H + it.h) * (D * D)), "n"(D * D * 4) : "memory");
             __syncwarp();
             const int v0 = it.slice * NV;
             for (int c = 0; c < it.n_chunks; c++, rt.next()) {
@@ -544,11 +632,12 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
         Ring<2> rna, rp, ru;          // A of chunk n + 1, A and P of chunk n, sums
         Ring<OUTS> rs;
         Ring<OB> rb;
-        bool alive = true;
+        bool alive = true, kept = false;          // kept: the state behind the item's last chunk is wanted
         auto next_item = [&]() {                  // its chunks, or 0: there are no more
             for (;;) {
                 if (!(alive = wait(&m.item_full[ri.i], ri.ph))) return 0;
                 const int seq = m.items[ri.i].seq, chunks = m.items[ri.i].n_chunks;
+                if (GEN) kept = m.items[ri.i].out >= 0;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.item_empty[ri.i]);
                 ri.next();
@@ -584,6 +673,8 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                 if (step) {
                     if (elect_one()) {
                         mma_steps<4, MN, MN, 0, 0>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(tile + S::K), desc_lo_mn<BT>(tile + S::V), IDESC_U);
+                        if constexpr (GEN)
+                            mma_steps<4, MN, MN, 0, 0, true>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(base + S::lo), desc_lo_mn<BT>(tile + S::V), IDESC_U);
                         mma_commit(&m.u_full[ru.i]);
                     }
                     __syncwarp();
@@ -609,7 +700,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                 product_a();
             }
             begun = more;                         // chunk n + 1 is the next round's n
-            step = more && left > 1;
+            step = more && (left > 1 || kept);
             if (more && --left == 0) left = next_item();
             more = left > 0;
         }
@@ -672,6 +763,22 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                 if (c < 0) continue;
                 asm volatile("cp.async.wait_group 5;" ::: "memory");
                 float y[2] = {m.raw[c % RAW][lane] * LOG2E, m.raw[c % RAW][lane + 32] * LOG2E};
+                float z[2] = {y[0], y[1]};        // GEN: what decays a row's key until the chunk's end, summed from there (a difference of
+                if constexpr (GEN) {              // running sums would lose it behind a strong decay)
+#pragma unroll
+                    for (int s = 1; s < 32; s <<= 1) {
+                        const float z0 = __shfl_down_sync(~0u, z[0], s), z1 = __shfl_down_sync(~0u, z[1], s);
+                        if (lane + s < 32) {
+                            z[0] += z0;
+                            z[1] += z1;
+                        }
+                    }
+                    const float upper = __shfl_sync(~0u, z[1], 0);
+                    z[0] = __shfl_down_sync(~0u, z[0], 1);
+                    z[1] = __shfl_down_sync(~0u, z[1], 1);
+                    if (lane == 31) z[0] = z[1] = 0.f;
+                    z[0] += upper;
+                }
 #pragma unroll
                 for (int s = 1; s < 32; s <<= 1) {
                     const float y0 = __shfl_up_sync(~0u, y[0], s), y1 = __shfl_up_sync(~0u, y[1], s);
@@ -689,8 +796,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                     const int t = lane + 32 * u, vr = c * BT + t;
                     rd.nb2[t] = -y[u];
                     rd.eb[t] = ex2(y[u]);
-                    rd.w[t] = split_weight(ex2(bn - y[u]));
-                    rd.code[t] = vr >= it.n_replay && vr < it.n_virtual ? it.own_begin + vr - it.n_replay : -1;
+                    if constexpr (GEN) rd.w[t].x = __float_as_uint(ex2(z[u]));
+                    else rd.w[t] = split_weight(ex2(bn - y[u]));
+                    rd.code[t] = (!GEN || o) && vr >= it.n_replay && vr < it.n_virtual ? it.own_begin + vr - it.n_replay : -1;
                 }
                 rd.part[lane] = ex2(bh - y[0]);
                 rd.part[32 + lane] = ex2(y[1] - bh);
@@ -699,8 +807,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
                     rd.h = it.h;
                     rd.col0 = it.slice * NV;
                     rd.row0 = it.own_begin - it.n_replay + c * BT;
-                    rd.full = (c > 0 || it.n_replay == 0) && (c + 1) * BT <= it.n_virtual;
-                    rd.step = c + 1 < it.n_chunks;
+                    rd.full = (!GEN || o) && (c > 0 || it.n_replay == 0) && (c + 1) * BT <= it.n_virtual;
+                    rd.step = c + 1 < it.n_chunks || it.out >= 0;
+                    if (GEN) rd.valid = min(BT, it.n_virtual - c * BT);
                     rd.end = 0;
                 }
                 __syncwarp();
@@ -762,7 +871,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, cons
 
 template <int NV>
 int32_t launch(const FwdArgs& a, int* flags, int* ticket) {
-    using S = Shape<NV>;
+    using S = Shape<NV, false>;
     CUtensorMap mq, mk, mv, mcs, mo;
     int32_t rc;
     if ((rc = make_row_map(&mq, a.q, a.tb.n_rows, a.H)) != HARTS_OK) return rc;
@@ -771,15 +880,38 @@ int32_t launch(const FwdArgs& a, int* flags, int* ticket) {
     if ((rc = make_row_map(&mo, a.o, a.tb.n_rows, a.H)) != HARTS_OK) return rc;
     const void* cs = a.chunk_states ? a.chunk_states : a.q;   // a valid address for the (unused) map
     if ((rc = make_state_map(&mcs, cs, a.chunk_states ? (int64_t)a.tb.n_chunks * a.H : 1)) != HARTS_OK) return rc;
-    if (cudaFuncSetAttribute(pipe_fwd_kernel<NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    if (cudaFuncSetAttribute(pipe_fwd_kernel<NV, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
     const int n = (a.seq_hi - a.seq_lo) * a.H * (D / NV);
-    pipe_fwd_kernel<NV><<<n < sm_count() ? n : sm_count(), NT, S::bytes, a.stream>>>(
-        a.tb, a.seq_lo, n, a.H, mq, mk, mv, mcs, mo, (const __nv_bfloat16*)a.q, (const __nv_bfloat16*)a.k, (const __nv_bfloat16*)a.v, a.g,
+    pipe_fwd_kernel<NV, false><<<n < sm_count() ? n : sm_count(), NT, S::bytes, a.stream>>>(
+        a.tb, GenItems{}, a.seq_lo, n, a.H, mq, mk, mv, mcs, mo, (const __nv_bfloat16*)a.q, (const __nv_bfloat16*)a.k, (const __nv_bfloat16*)a.v, a.g,
         (__nv_bfloat16*)a.o, a.slots, a.chunk_states != nullptr, a.dev_status, status_gate(a.flags, a.dev_status), flags, ticket);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
 
+template <int NV>
+int32_t launch_gen(const GenLaArgs& a, const GenItems& items, int64_t max_items) {
+    using S = Shape<NV, true>;
+    CUtensorMap mq, mk, mv, mo;
+    int32_t rc;
+    const int rows = (int)a.n_rows;
+    // without outputs the queries are not needed: any rows in their place
+    if ((rc = make_row_map_ld(&mq, a.o ? a.q : a.k, rows, a.H, a.o ? a.ld_q : a.ld_k)) != HARTS_OK) return rc;
+    if ((rc = make_row_map_ld(&mk, a.k, rows, a.H, a.ld_k)) != HARTS_OK) return rc;
+    if ((rc = make_row_map_ld(&mv, a.v, rows, a.H, a.ld_v)) != HARTS_OK) return rc;
+    if ((rc = make_row_map(&mo, a.o ? a.o : a.k, rows, a.H)) != HARTS_OK) return rc;
+    if (cudaFuncSetAttribute(pipe_fwd_kernel<NV, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    const int64_t n = max_items * a.H * (D / NV);
+    return launch_after(pipe_fwd_kernel<NV, true>, n < sm_count() ? (int)n : sm_count(), NT, S::bytes, a.stream, harts_la_tables_t{}, items, 0, 0, a.H,
+                        mq, mk, mv, mq, mo, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, a.g,
+                        (__nv_bfloat16*)a.o, a.states, 0, a.dev_status, (const int32_t*)nullptr, (int*)nullptr, (int*)nullptr) == cudaSuccess
+               ? HARTS_OK : HARTS_ECUDA;
+}
+
 }  // namespace
+
+int32_t pipe_gen(const GenLaArgs& a, const GenItems& items, int64_t max_items) {
+    return 2 * max_items * a.H <= sm_count() ? launch_gen<64>(a, items, max_items) : launch_gen<128>(a, items, max_items);
+}
 
 // flags == nullptr: sequences [a.seq_lo, a.seq_hi) of one round; otherwise all rounds in one launch (first_round: sequences of the first):
 // the CTAs draw the (sequence, head, slice) items from a ticket counter in the plan's order, and one that starts from an exported

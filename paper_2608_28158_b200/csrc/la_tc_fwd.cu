@@ -522,15 +522,17 @@ int32_t encode(Args... args) {
 
 }  // namespace
 
-// [rows][H][128] bf16 tensor, box = 64 rows x 1 head x 64 columns
-int32_t make_row_map(CUtensorMap* map, const void* base, int64_t rows, int32_t H) {
+// [rows][H][128] bf16 tensor with ld elements between rows, box = 64 rows x 1 head x 64 columns
+int32_t make_row_map_ld(CUtensorMap* map, const void* base, int64_t rows, int32_t H, int64_t ld) {
     cuuint64_t dims[3] = {128, (cuuint64_t)H, (cuuint64_t)rows};
-    cuuint64_t strides[2] = {256, (cuuint64_t)H * 256};
+    cuuint64_t strides[2] = {256, (cuuint64_t)ld * 2};
     cuuint32_t box[3] = {64, 1, 64}, es[3] = {1, 1, 1};
     return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
+
+int32_t make_row_map(CUtensorMap* map, const void* base, int64_t rows, int32_t H) { return make_row_map_ld(map, base, rows, H, (int64_t)H * 128); }
 
 // [n][128][128] bf16 states, box = 1 state x 128 rows x 64 columns
 int32_t make_state_map(CUtensorMap* map, const void* base, int64_t n) {
