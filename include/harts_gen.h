@@ -61,6 +61,66 @@ int32_t harts_gen_la(int32_t n_seq, const int32_t* seq_begin, const int32_t* seq
                      int32_t dk, int32_t dv, int32_t dtype, void* workspace, size_t workspace_bytes, int32_t* dev_status,
                      void* stream);
 
+/*
+ * Paged cache of keys and values, d = 128.
+ *   k_cache, v_cache [n_pages, Hkv, page, 128]: a token's row lies in slot = page number * page + place in the page; page is 16, 32,
+ *   64 or 128, n_pages * page and n_pages * Hkv at most INT32_MAX
+ *   cache_type HARTS_BF16: the rows as they are; k_exp, v_exp NULL
+ *   cache_type HARTS_E4M3: 8-bit values y with a power of two for each (token, head): row = y 2^(exp - 127), exp in k_exp, v_exp
+ *              uint8 [n_pages, Hkv, page].  The power is the smallest with max |row| <= 448 2^e (not below 2^-126), so that y is the row's
+ *              values rounded to 4 significant bits, to nearest even, whatever their size, and reading back is exact (what would round to
+ *              2^128 becomes the value below it).  A row with an infinity
+ *              or a NaN becomes all NaN: exp 255, values zero.
+ *
+ * harts_gen_cache_write: rows of k, v (bf16 [n, Hkv, 128], heads contiguous, ld_k, ld_v elements between rows) into slots slot[i]
+ * (device int32 [n]); slot[i] < 0: the row is left out (a padded batch).  Two rows of a call have different slots (or what stays
+ * is undefined).  A slot beyond the cache is left out and reported.
+ * harts_gen_cache_read: the rows of slots slot[i] into k, v (bf16 [n, Hkv, 128], contiguous); slot[i] < 0 and slots beyond the cache
+ * (reported) give zeros.  Either of k, v may be NULL.
+ */
+#define HARTS_E4M3 2
+int32_t harts_gen_cache_write(int64_t n, const int32_t* slot, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* k_cache,
+                              void* v_cache, uint8_t* k_exp, uint8_t* v_exp, int32_t n_pages, int32_t page, int32_t Hkv, int32_t d,
+                              int32_t cache_type, int32_t* dev_status, void* stream);
+int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache, const void* v_cache, const uint8_t* k_exp,
+                             const uint8_t* v_exp, void* k, void* v, int32_t n_pages, int32_t page, int32_t Hkv, int32_t d,
+                             int32_t cache_type, int32_t* dev_status, void* stream);
+
+/*
+ * Attention of sampled tokens on the cached tree.  The cached forest is given like a training forest (tree_node_ptr, node_parent,
+ * node_fork_off, node_len as for harts_la_plan(), but node_len may be 0 and a fork offset anything from 0 to its parent's length); node
+ * v's token j is in slot node_page[node_page_ptr[v] + j / page] * page + j % page of the cache.  Query r belongs to node q_node[r] and
+ * sees that node's tokens 0 .. q_pos[r] and, of every ancestor, the tokens ahead of the fork:
+ *
+ *     o_r = sum_j softmax_j(scale q_r . k_j) v_j,     lse_r = log sum_j exp(scale q_r . k_j)     (per query head; kv head = head / (Hq / Hkv))
+ *
+ * A branch that decodes one token has one query (its newest token, whose key is in the cache already); drafted tokens are more queries
+ * of the same node.  q_node[r] < 0, and a query that sees nothing: o = 0, lse = -inf.  Stored tokens that a query does not see may hold anything,
+ * infinities and NaN too.
+ *
+ * harts_gen_attn_index (host in, host out): work lists for such a forest, one int32 blob; the same blob is copied to the device.
+ *   Tokens that several queries see are read once for up to 128 rows (a row: a query and a head of its group), long runs are split over the GPU.
+ *   grow: by how many tokens nodes with queries may grow while the index is used: between calls (and replays of a captured call) q_pos may
+ *   go up, to node_len - 1 + grow at most, and never below what it was for the index.  node_page has to list the pages of that many tokens.
+ *   A new branch, a fork, or a query more or less needs a new index.
+ *   cap_words: capacity of blob, which may be NULL to get *n_words only.
+ *   Errors: HARTS_EINVAL (malformed forest, pages missing or negative, q_pos out of range, capacity), HARTS_ENOMEM.
+ * harts_gen_attn_workspace_bytes: of the parts of split sums.  Calls that share a workspace must not run at the same time.
+ * harts_gen_attn: q bf16 [n_q, Hq, 128], heads contiguous, ld_q elements between rows; q_pos device int32 [n_q]; o bf16, lse fp32,
+ *   contiguous, written for every query.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
+ *   Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
+ */
+#define HARTS_GEN_ATTN_HEADER_WORDS 32
+int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_node_ptr, const int32_t* node_parent, const int32_t* node_fork_off,
+                             const int32_t* node_len, const int32_t* node_page_ptr, const int32_t* node_page, int32_t page, int32_t n_q,
+                             const int32_t* q_node, const int32_t* q_pos, int32_t Hq, int32_t Hkv, int32_t grow, int64_t cap_words,
+                             int32_t* blob, int64_t* n_words);
+int32_t harts_gen_attn_workspace_bytes(const int32_t* host_index, size_t* bytes);
+int32_t harts_gen_attn(const int32_t* host_index, const int32_t* dev_index, const void* q, int64_t ld_q, const void* k_cache,
+                       const void* v_cache, const uint8_t* k_exp, const uint8_t* v_exp, int32_t n_pages, int32_t cache_type,
+                       const int32_t* q_pos, void* o, float* lse, float scale, void* workspace, size_t workspace_bytes,
+                       int32_t* dev_status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

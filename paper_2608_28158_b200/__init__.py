@@ -16,4 +16,6 @@ from .logp import (  # noqa: F401
 from .conv import harts_conv_index, harts_conv_fwd, harts_conv_scratch_bytes, harts_conv_bwd  # noqa: F401
 from .attn import AttnIndex, harts_attn_index, harts_attn_fwd, harts_attn_bwd  # noqa: F401
 from .mb import MbPlan, harts_mb_plan  # noqa: F401
-from .gen import harts_gen_la_workspace_bytes, harts_gen_la  # noqa: F401
+from .gen import (  # noqa: F401
+    HARTS_E4M3, GenAttnIndex, harts_gen_la_workspace_bytes, harts_gen_la, harts_gen_cache_write, harts_gen_cache_read, harts_gen_attn_index, harts_gen_attn,
+)

@@ -78,4 +78,72 @@ int32_t harts_gen_la(int32_t n_seq, const int32_t* seq_begin, const int32_t* seq
     return harts::gen_la_chunks(a);
 }
 
+// ---- cache ---------------------------------------------------------------------------------------------------------------------
+static int32_t cache_check(int64_t n, int32_t n_pages, int32_t page, int32_t Hkv, int32_t d, int32_t type) {
+    if (type != HARTS_BF16 && type != HARTS_E4M3) return HARTS_EUNSUPPORTED;
+    if (d != 128) return HARTS_EUNSUPPORTED;
+    if (n < 0 || n > INT32_MAX || n_pages < 0 || Hkv < 1 || Hkv > 65535 || (page != 16 && page != 32 && page != 64 && page != 128)) return HARTS_EINVAL;
+    if ((int64_t)n_pages * page > INT32_MAX || (int64_t)n_pages * Hkv > INT32_MAX) return HARTS_EINVAL;
+    return HARTS_OK;
+}
+static bool cache_ok(const harts::GenCache& c) {
+    if (c.n_pages == 0) return true;
+    if (!c.k || !c.v || !aligned16(c.k) || !aligned16(c.v)) return false;
+    return c.type == HARTS_BF16 || (c.k_exp && c.v_exp && aligned16(c.k_exp) && aligned16(c.v_exp));
+}
+
+int32_t harts_gen_cache_write(int64_t n, const int32_t* slot, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* k_cache,
+                              void* v_cache, uint8_t* k_exp, uint8_t* v_exp, int32_t n_pages, int32_t page, int32_t Hkv, int32_t d,
+                              int32_t cache_type, int32_t* dev_status, void* stream) {
+    const int32_t rc = cache_check(n, n_pages, page, Hkv, d, cache_type);
+    if (rc != HARTS_OK) return rc;
+    const harts::GenCache c{k_cache, v_cache, k_exp, v_exp, n_pages, page, Hkv, cache_type};
+    if (n == 0) return HARTS_OK;
+    if (!slot || !cache_ok(c) || !rows_ok(k, ld_k, (int64_t)Hkv * d, 2) || !rows_ok(v, ld_v, (int64_t)Hkv * d, 2)) return HARTS_EINVAL;
+    return harts::gen_cache_write(c, {n, slot, const_cast<void*>(k), const_cast<void*>(v), ld_k, ld_v, dev_status, static_cast<cudaStream_t>(stream)});
+}
+
+int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache, const void* v_cache, const uint8_t* k_exp,
+                             const uint8_t* v_exp, void* k, void* v, int32_t n_pages, int32_t page, int32_t Hkv, int32_t d,
+                             int32_t cache_type, int32_t* dev_status, void* stream) {
+    const int32_t rc = cache_check(n, n_pages, page, Hkv, d, cache_type);
+    if (rc != HARTS_OK) return rc;
+    const harts::GenCache c{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<uint8_t*>(k_exp), const_cast<uint8_t*>(v_exp),
+                            n_pages, page, Hkv, cache_type};
+    if (n == 0 || (!k && !v)) return HARTS_OK;
+    if (!slot || !cache_ok(c) || !aligned16(k) || !aligned16(v)) return HARTS_EINVAL;
+    return harts::gen_cache_read(c, {n, slot, k, v, 0, 0, dev_status, static_cast<cudaStream_t>(stream)});
+}
+
+// ---- attention -------------------------------------------------------------------------------------------------------------------
+static bool index_ok(const int32_t* hi) {
+    using namespace harts::gen_attn;
+    return hi && hi[N_Q] >= 0 && hi[HKV] >= 1 && hi[HQ] >= hi[HKV] && hi[WORDS] >= HARTS_GEN_ATTN_HEADER_WORDS && hi[N_PARTS] >= 0;
+}
+
+int32_t harts_gen_attn_workspace_bytes(const int32_t* host_index, size_t* bytes) {
+    using namespace harts::gen_attn;
+    if (!bytes || !index_ok(host_index)) return HARTS_EINVAL;
+    *bytes = host_index[MERGED] ? (size_t)host_index[N_PARTS] * host_index[HKV] * (128 + 1) * sizeof(float) : 0;
+    return HARTS_OK;
+}
+
+int32_t harts_gen_attn(const int32_t* host_index, const int32_t* dev_index, const void* q, int64_t ld_q, const void* k_cache,
+                       const void* v_cache, const uint8_t* k_exp, const uint8_t* v_exp, int32_t n_pages, int32_t cache_type,
+                       const int32_t* q_pos, void* o, float* lse, float scale, void* workspace, size_t workspace_bytes,
+                       int32_t* dev_status, void* stream) {
+    using namespace harts::gen_attn;
+    size_t need = 0;
+    if (harts_gen_attn_workspace_bytes(host_index, &need) != HARTS_OK || !dev_index || !aligned16(dev_index) || !(scale > 0.f)) return HARTS_EINVAL;
+    const int32_t rc = cache_check(host_index[N_Q], n_pages, host_index[PAGE], host_index[HKV], 128, cache_type);
+    if (rc != HARTS_OK) return rc;
+    if (host_index[N_Q] == 0) return HARTS_OK;
+    const harts::GenCache c{const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<uint8_t*>(k_exp), const_cast<uint8_t*>(v_exp),
+                            n_pages, host_index[PAGE], host_index[HKV], cache_type};
+    if (host_index[MAX_PAGE] >= n_pages || !cache_ok(c) || !q_pos || !o || !lse || !aligned16(o) || !rows_ok(q, ld_q, (int64_t)host_index[HQ] * 128, 2))
+        return HARTS_EINVAL;
+    if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return HARTS_EINVAL;
+    return harts::gen_attn_launch(host_index, dev_index, q, ld_q, c, q_pos, o, lse, scale, workspace, dev_status, static_cast<cudaStream_t>(stream));
+}
+
 }  // extern "C"

@@ -1,0 +1,229 @@
+// Host index for the attention of sampled tokens on the cached tree: which queries see which tokens of a node, cut into units of
+// work (rows x a run of tokens) for the two kernels, and where the parts of a query's sum are.
+//
+// A node's tokens are seen by its own queries, up to their positions, and by those of every branch below a fork, up to the fork.  Runs of tokens
+// between such limits are read once for all queries that see them; limits that lie within MIXED tokens of each other are taken
+// together, and the narrow kernel then looks at every row's own limit.  A node that only its own queries see is one run.
+#include <algorithm>
+#include <cstdint>
+#include <new>
+#include <vector>
+
+#include "gen.h"
+
+namespace {
+
+using namespace harts::gen_attn;
+
+constexpr int TILE = 64;
+constexpr bool HAVE_WIDE = false;
+constexpr int MIXED = 2 * TILE;         // limits this near to each other share a run
+constexpr int LEAST = 256;              // tokens a unit is not cut below
+constexpr int CTAS = 148 * 3;           // units wanted, all key heads together
+
+struct Range {
+    int node, a, b, entry, n_entries;
+    bool wide;
+};
+struct Index {
+    std::vector<Unit> narrow, wide;
+    std::vector<Entry> entries;
+    std::vector<int32_t> part_ptr, part;
+    int32_t n_parts = 0, merged = 0, max_page = -1;
+};
+
+bool forest_ok(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const int32_t* off, const int32_t* len) {
+    if (ptr[0] != 0) return false;
+    for (int32_t t = 0; t < n_trees; t++) {
+        const int32_t lo = ptr[t], hi = ptr[t + 1];
+        if (hi <= lo) return false;
+        for (int32_t i = lo; i < hi; i++) {
+            if (len[i] < 0) return false;
+            if (i == lo ? (parent[i] != -1 || off[i] != 0) : (parent[i] < 0 || parent[i] >= i - lo || off[i] < 0 || off[i] > len[lo + parent[i]])) return false;
+        }
+    }
+    return true;
+}
+
+int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const int32_t* off, const int32_t* len, const int32_t* page_ptr,
+              const int32_t* pages, int32_t page, int32_t n_q, const int32_t* q_node, const int32_t* q_pos, int32_t Hq, int32_t Hkv, int32_t grow,
+              Index& ix) {
+    const int32_t n_nodes = ptr[n_trees], G = Hq / Hkv;
+    struct Sees {
+        int32_t row, limit;              // -1: its own node
+    };
+    std::vector<std::vector<Sees>> sees(n_nodes);
+    std::vector<int32_t> base(n_nodes);
+    for (int32_t t = 0; t < n_trees; t++)
+        for (int32_t i = ptr[t]; i < ptr[t + 1]; i++) base[i] = ptr[t];
+    for (int32_t r = 0; r < n_q; r++) {
+        if (q_node[r] < 0) continue;
+        if (q_node[r] >= n_nodes || q_pos[r] < -1 || q_pos[r] >= len[q_node[r]]) return HARTS_EINVAL;
+        int32_t v = q_node[r];
+        sees[v].push_back({r, -1});
+        for (; parent[v] >= 0; v = base[v] + parent[v])
+            if (off[v] > 0) sees[base[v] + parent[v]].push_back({r, off[v]});
+    }
+    std::vector<Range> ranges;
+    std::vector<int32_t> parts_of(n_q, 0);
+    auto add = [&](int node, int a, int b, bool wide, const std::vector<Entry>& e) {
+        if (e.empty() || b <= a) return;
+        ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), HAVE_WIDE && wide && (int64_t)e.size() * G > NARROW_ROWS});
+        ix.entries.insert(ix.entries.end(), e.begin(), e.end());
+    };
+    std::vector<Entry> e;
+    for (int32_t v = 0; v < n_nodes; v++) {
+        auto& s = sees[v];
+        int n_own = 0;
+        int64_t least = INT32_MAX;
+        for (const Sees& x : s)
+            if (x.limit < 0) {
+                n_own++;
+                least = std::min<int64_t>(least, q_pos[x.row] + 1);
+            }
+        const int64_t most = (int64_t)len[v] + (n_own ? grow : 0);
+        if (most >= INT32_MAX - TILE || page_ptr[v + 1] < page_ptr[v] || (most + page - 1) / page > page_ptr[v + 1] - page_ptr[v]) return HARTS_EINVAL;
+        for (int32_t p = page_ptr[v]; p < page_ptr[v + 1]; p++) {
+            if (pages[p] < 0) return HARTS_EINVAL;
+            ix.max_page = std::max(ix.max_page, pages[p]);
+        }
+        if (s.empty()) continue;
+        // what its own queries see for certain, in whole tiles, is shared with the branches below; a node of few rows alone is one run
+        int own_from = 0;
+        if (n_own && (n_own < (int)s.size() || (int64_t)n_own * G > NARROW_ROWS)) own_from = (int)(least / TILE * TILE);
+        std::vector<int32_t> limits;
+        for (Sees& x : s) {
+            const int32_t l = x.limit < 0 ? own_from : x.limit;
+            if (l > 0) limits.push_back(l);
+        }
+        std::sort(limits.begin(), limits.end());
+        limits.erase(std::unique(limits.begin(), limits.end()), limits.end());
+        auto seeing = [&](int from, int to) {           // queries that see tokens behind `from`, up to `to` at most
+            e.clear();
+            for (const Sees& x : s) {
+                const int32_t l = x.limit < 0 ? own_from : x.limit;
+                if (l > from) e.push_back({x.row, std::min(l, to), 0, 0});
+            }
+        };
+        int a = 0;
+        for (size_t i = 0; i < limits.size();) {
+            if (limits[i] - a > MIXED || i + 1 == limits.size()) {
+                seeing(a, limits[i]);
+                add(v, a, limits[i], true, e);
+                a = limits[i++];
+                continue;
+            }
+            size_t j = i;
+            while (j + 1 < limits.size() && limits[j + 1] - a <= MIXED) j++;
+            seeing(a, limits[j]);
+            add(v, a, limits[j], j == i, e);
+            a = limits[j];
+            i = j + 1;
+        }
+        if (n_own) {
+            e.clear();
+            for (const Sees& x : s)
+                if (x.limit < 0) e.push_back({x.row, -1, own_from, (int32_t)most});
+            add(v, own_from, (int)most, false, e);
+        }
+    }
+    // cut long runs: as many units as keep the GPU busy, none shorter than LEAST
+    int64_t total = 0;
+    auto units_of = [&](const Range& r) {
+        const int64_t rows = (int64_t)r.n_entries * G;
+        return (rows + (r.wide ? WIDE_ROWS : NARROW_ROWS) - 1) / (r.wide ? WIDE_ROWS : NARROW_ROWS);
+    };
+    for (const Range& r : ranges) total += units_of(r) * (r.b - r.a) * Hkv;
+    const int64_t cut = std::max<int64_t>(LEAST, (total + CTAS - 1) / CTAS);
+    std::stable_sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.b - x.a > y.b - y.a; });
+    std::vector<std::vector<int32_t>> parts(n_q);
+    int64_t n_parts = 0;
+    for (const Range& r : ranges) {
+        const int64_t n = r.b - r.a, rows = (int64_t)r.n_entries * G, per = r.wide ? WIDE_ROWS : NARROW_ROWS;
+        const int64_t pieces = (n + cut - 1) / cut;
+        for (int64_t p = 0; p < pieces; p++) {
+            auto edge = [&](int64_t i) { return (int32_t)(i <= 0 ? r.a : i >= pieces ? r.b : std::max<int64_t>(r.a, (r.a + n * i / pieces) / TILE * TILE)); };
+            const int32_t k0 = edge(p), k1 = edge(p + 1);
+            if (k1 <= k0) continue;
+            for (int64_t f = 0; f < rows; f += per)
+                (r.wide ? ix.wide : ix.narrow).push_back({r.entry, (int32_t)f, (int32_t)std::min(per, rows - f), k0, k1, page_ptr[r.node], (int32_t)n_parts, 0});
+            for (int i = 0; i < r.n_entries; i++) parts[ix.entries[r.entry + i].row].push_back((int32_t)(n_parts + (int64_t)i * G));
+            n_parts += rows;
+            if (n_parts > INT32_MAX - (1 << 20)) return HARTS_EINVAL;
+        }
+    }
+    ix.n_parts = (int32_t)n_parts;
+    auto longer = [](const Unit& x, const Unit& y) { return x.k1 - x.k0 > y.k1 - y.k0; };
+    std::stable_sort(ix.narrow.begin(), ix.narrow.end(), longer);
+    std::stable_sort(ix.wide.begin(), ix.wide.end(), longer);
+    ix.part_ptr.assign(1, 0);
+    for (int32_t r = 0; r < n_q; r++) {
+        if (parts[r].size() == 1) parts[r][0] = -1;               // written by its unit
+        else ix.merged = 1;
+        ix.part.insert(ix.part.end(), parts[r].begin(), parts[r].end());
+        ix.part_ptr.push_back((int32_t)ix.part.size());
+    }
+    for (Entry& x : ix.entries)
+        if (parts[x.row].size() == 1) x.most = -x.most - 1;
+    return HARTS_OK;
+}
+
+}  // namespace
+
+extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_node_ptr, const int32_t* node_parent,
+                                        const int32_t* node_fork_off, const int32_t* node_len, const int32_t* node_page_ptr,
+                                        const int32_t* node_page, int32_t page, int32_t n_q, const int32_t* q_node, const int32_t* q_pos,
+                                        int32_t Hq, int32_t Hkv, int32_t grow, int64_t cap_words, int32_t* blob, int64_t* n_words) {
+    if (n_trees < 0 || n_q < 0 || grow < 0 || !tree_node_ptr || !node_page_ptr || !n_words || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 ||
+        (page != 16 && page != 32 && page != 64 && page != 128))
+        return HARTS_EINVAL;
+    if (tree_node_ptr[0] != 0 || tree_node_ptr[n_trees] < 0 || node_page_ptr[0] != 0) return HARTS_EINVAL;
+    if (tree_node_ptr[n_trees] > 0 && (!node_parent || !node_fork_off || !node_len)) return HARTS_EINVAL;
+    if (n_q > 0 && (!q_node || !q_pos)) return HARTS_EINVAL;
+    try {
+        if (!forest_ok(n_trees, tree_node_ptr, node_parent, node_fork_off, node_len)) return HARTS_EINVAL;
+        if (node_page_ptr[tree_node_ptr[n_trees]] > 0 && !node_page) return HARTS_EINVAL;
+        Index ix;
+        const int32_t rc = build(n_trees, tree_node_ptr, node_parent, node_fork_off, node_len, node_page_ptr, node_page, page, n_q, q_node, q_pos, Hq, Hkv,
+                                 grow, ix);
+        if (rc != HARTS_OK) return rc;
+        const int64_t n_pages = node_page_ptr[tree_node_ptr[n_trees]];
+        int64_t total = HARTS_GEN_ATTN_HEADER_WORDS, at[6];
+        const int64_t sizes[6] = {(int64_t)(ix.narrow.size() * sizeof(Unit) / 4), (int64_t)(ix.wide.size() * sizeof(Unit) / 4),
+                                  (int64_t)(ix.entries.size() * sizeof(Entry) / 4), n_pages, n_q + 1, (int64_t)ix.part.size()};
+        for (int i = 0; i < 6; i++) {
+            at[i] = total;
+            total += (sizes[i] + 3) & ~int64_t(3);            // 16-byte aligned starts
+        }
+        if (total >= INT32_MAX) return HARTS_EINVAL;
+        *n_words = total;
+        if (!blob) return HARTS_OK;
+        if (cap_words < total) return HARTS_EINVAL;
+        std::fill(blob, blob + total, 0);
+        blob[N_Q] = n_q;
+        blob[HQ] = Hq;
+        blob[HKV] = Hkv;
+        blob[PAGE] = page;
+        blob[N_NARROW] = (int32_t)ix.narrow.size();
+        blob[N_WIDE] = (int32_t)ix.wide.size();
+        blob[N_PARTS] = ix.n_parts;
+        blob[MERGED] = ix.merged;
+        blob[MAX_PAGE] = ix.max_page;
+        blob[WORDS] = (int32_t)total;
+        for (int i = 0; i < 6; i++) blob[NARROW + i] = (int32_t)at[i];
+        auto put = [&](int i, const void* p, int64_t words) {
+            if (words) std::copy_n(static_cast<const int32_t*>(p), words, blob + at[i]);
+        };
+        put(0, ix.narrow.data(), sizes[0]);
+        put(1, ix.wide.data(), sizes[1]);
+        put(2, ix.entries.data(), sizes[2]);
+        put(3, node_page, sizes[3]);
+        put(4, ix.part_ptr.data(), sizes[4]);
+        put(5, ix.part.data(), sizes[5]);
+    } catch (const std::bad_alloc&) {
+        return HARTS_ENOMEM;
+    } catch (...) {
+        return HARTS_EINTERNAL;
+    }
+    return HARTS_OK;
+}

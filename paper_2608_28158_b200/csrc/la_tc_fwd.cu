@@ -534,6 +534,15 @@ int32_t make_row_map_ld(CUtensorMap* map, const void* base, int64_t rows, int32_
 
 int32_t make_row_map(CUtensorMap* map, const void* base, int64_t rows, int32_t H) { return make_row_map_ld(map, base, rows, H, (int64_t)H * 128); }
 
+// pages of a cache, [n][page][128] bf16 or bytes: box = up to 64 rows of a page x 128 bytes
+int32_t make_cache_map(CUtensorMap* map, const void* base, int64_t n, int32_t page, bool bytes) {
+    const cuuint64_t row = bytes ? 128 : 256;
+    cuuint64_t dims[3] = {128, (cuuint64_t)page, (cuuint64_t)n}, strides[2] = {row, row * page};
+    cuuint32_t box[3] = {bytes ? 128u : 64u, page < 64 ? (cuuint32_t)page : 64u, 1}, es[3] = {1, 1, 1};
+    return encode(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 // [n][128][128] bf16 states, box = 1 state x 128 rows x 64 columns
 int32_t make_state_map(CUtensorMap* map, const void* base, int64_t n) {
     cuuint64_t dims[3] = {128, 128, (cuuint64_t)(n < 1 ? 1 : n)};

@@ -1,0 +1,322 @@
+"""harts_gen_attn on the GPU: attention of sampled tokens on a cached tree against its definition, query by query in 64 bits."""
+import math
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_28158_b200 as H
+
+pytestmark = pytest.mark.gpu
+
+
+class Tree:
+    """A cached forest in random pages; all other places of the pages hold NaN (bf16) or any bytes (8 bits)."""
+
+    def __init__(self, ptr, par, off, ln, page, hkv, kind, seed, grow=0, spare=3, scale=1.0):
+        rng = random.Random(seed)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(seed)
+        self.ptr, self.par, self.off, self.len, self.page, self.hkv, self.kind, self.grow = ptr, par, off, ln, page, hkv, kind, grow
+        counts = [-(-(n + grow) // page) for n in ln]
+        order = list(range(sum(counts) + spare))
+        rng.shuffle(order)
+        self.page_ptr, self.pages, n_pages = np.concatenate([[0], np.cumsum(counts)]), order[:sum(counts)], len(order)
+        slots = []
+        for v, n in enumerate(ln):
+            at = np.asarray(self.pages[self.page_ptr[v]:self.page_ptr[v + 1]], dtype=np.int64)
+            j = np.arange(n + grow)
+            slots.append(torch.as_tensor(at[j // page] * page + j % page if n + grow else np.zeros(0, np.int64)).cuda())
+        self.slots = slots
+        self.exp = [None, None]
+        self.cache, self.values = [], []
+        for i in range(2):
+            x = torch.randn(n_pages, hkv, page, 128, generator=gen, device="cuda") * scale
+            if kind == "bf16":
+                c = x.to(torch.bfloat16)
+                c.view(-1)[torch.randint(0, 3, (c.numel(),), generator=gen, device="cuda") == 0] += 0
+                used = torch.zeros(n_pages, page, dtype=torch.bool, device="cuda")
+                for v, n in enumerate(ln):
+                    s = slots[v][:n + grow]
+                    used[s // page, s % page] = True
+                c.transpose(1, 2)[~used] = float("nan") if i == 0 else float("inf")
+                self.cache.append(c)
+                self.values.append(c.double())
+            else:
+                c = (x * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+                e = torch.randint(117, 124, (n_pages, hkv, page), generator=gen, device="cuda").to(torch.uint8)
+                self.cache.append(c)
+                self.exp[i] = e
+                self.values.append(c.float().double() * (e.cpu().double() - 127).exp2().cuda()[..., None])
+
+    def index(self, q_node, q_pos, G):
+        return H.harts_gen_attn_index(self.ptr, self.par, self.off, self.len, self.page_ptr, self.pages, self.page, q_node, q_pos, G * self.hkv, self.hkv,
+                                      self.grow).upload()
+
+    def visible(self, v, p):
+        base = max(x for x in self.ptr if x <= v)
+        parts = [self.slots[v][:p + 1]]
+        while self.par[v] >= 0:
+            u = base + self.par[v]
+            parts.append(self.slots[u][:self.off[v]])
+            v = u
+        return torch.cat(parts)
+
+    def oracle(self, q, q_node, q_pos, scale):
+        n, hq, _ = q.shape
+        o = torch.zeros(n, hq, 128, dtype=torch.float64, device="cuda")
+        lse = torch.full((n, hq), -math.inf, dtype=torch.float64, device="cuda")
+        K, V = (x.transpose(1, 2).reshape(-1, self.hkv, 128) for x in self.values)
+        for r in range(n):
+            if q_node[r] < 0:
+                continue
+            at = self.visible(q_node[r], q_pos[r])
+            if len(at) == 0:
+                continue
+            s = torch.einsum("hgd,thd->hgt", q[r].double().view(self.hkv, -1, 128), K[at]) * scale
+            lse[r] = torch.logsumexp(s, -1).reshape(hq)
+            o[r] = torch.einsum("hgt,thd->hgd", torch.softmax(s, -1), V[at]).reshape(hq, 128)
+        return o, lse
+
+
+def run(tree, index, q, q_pos, scale, ws=None, stream=None):
+    n, hq, _ = q.shape
+    o = torch.full((n, hq, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((n, hq), float("nan"), device="cuda")
+    if ws is None:
+        ws = torch.full((max(16, index.workspace_bytes),), 255, dtype=torch.uint8, device="cuda")
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    pos = torch.tensor(q_pos, dtype=torch.int32, device="cuda")
+    H.harts_gen_attn(index, q, *tree.cache, pos, o, lse, scale, workspace=ws, k_exp=tree.exp[0], v_exp=tree.exp[1], dev_status=status, stream=stream)
+    return o, lse, status
+
+
+def queries(n, hq, seed, scale=1.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed + 1000)
+    return (torch.randn(n, hq, 128, generator=gen, device="cuda") * scale).to(torch.bfloat16)
+
+
+# A p is rounded to bf16 (off by 2^-9 of it at most) and so is the output, once (2^-9): 2 x 2^-9 = 2^-8 of the output's size where the p's
+# errors add up, which over rows of many values they do not.  lse: fp32 sums of bf16 products, 2^-24 a step over log terms: 2e-5 absolute.
+def compare(o, lse, ref_o, ref_lse):
+    none = torch.isneginf(ref_lse)
+    assert torch.equal(torch.isneginf(lse), none)
+    assert not o[none].any()
+    if (~none).any():
+        d = o.double()[~none] - ref_o[~none]
+        assert float(d.norm() / ref_o[~none].norm()) <= 2.0 ** -8
+        rows = d.norm(dim=-1) / ref_o[~none].norm(dim=-1)
+        assert float(rows.max()) <= 2.0 ** -6            # a row of few tokens: sums of a few rounded p's
+        assert float((lse.double() - ref_lse)[~none].abs().max()) <= 2e-5 * max(1.0, float(ref_lse[~none].abs().max()))
+
+
+def check(tree, q_node, q_pos, G, seed=0, later=None, scale=1 / math.sqrt(128), q_scale=1.0):
+    index = tree.index(q_node, q_pos, G)
+    q = queries(len(q_node), G * tree.hkv, seed, q_scale)
+    pos = list(q_pos) if later is None else later
+    o, lse, status = run(tree, index, q, pos, scale)
+    H.harts_la_check(status)
+    compare(o, lse, *tree.oracle(q, q_node, pos, scale))
+    return index
+
+
+KINDS = ["bf16", "e4m3"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("n", [1, 15, 16, 63, 64, 65, 129, 1000])
+def test_one_sequence(kind, page, n):
+    tree = Tree([0, 1], [-1], [0], [n], page, 2, kind, n)
+    check(tree, [0], [n - 1], 4, n)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("G,hkv", [(1, 1), (1, 5), (3, 2), (5, 1), (8, 4), (16, 1), (17, 2), (40, 1)])
+def test_head_layouts(kind, G, hkv):
+    tree = Tree([0, 4], [-1, 0, 0, 0], [0, 200, 200, 137], [200, 30, 71, 5], 32, hkv, kind, G)
+    check(tree, [1, 2, 3], [29, 70, 4], G, G)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches,prefix", [(2, 64), (7, 700), (33, 1025), (64, 333), (150, 4000)])
+def test_branches_of_a_prompt(kind, branches, prefix):
+    rng = random.Random(branches)
+    ln = [prefix] + [rng.randint(1, 300) for _ in range(branches)]
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [prefix] * branches, ln, 64, 2, kind, branches)
+    check(tree, list(range(1, branches + 1)), [n - 1 for n in ln[1:]], 4, branches)
+
+
+def any_forest(rng, trees, nodes, long=900):
+    ptr, par, off, ln = [0], [], [], []
+    for _ in range(trees):
+        t = [(-1, 0, rng.choice([0, 1, 63, 64, 500, long]))]
+        for i in range(1, nodes):
+            p = rng.randrange(i)
+            t.append((p, rng.randint(0, t[p][2]), rng.choice([0, 1, 2, 40, 64, 130, 300])))
+        par += [x[0] for x in t]
+        off += [x[1] for x in t]
+        ln += [x[2] for x in t]
+        ptr.append(len(par))
+    return ptr, par, off, ln
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("seed", range(8))
+def test_any_tree_with_drafts_and_padding(kind, seed):
+    rng = random.Random(seed)
+    ptr, par, off, ln = any_forest(rng, rng.randint(1, 3), rng.choice([3, 12, 30]))
+    tree = Tree(ptr, par, off, ln, rng.choice([16, 32, 64, 128]), rng.choice([1, 2]), kind, seed)
+    q_node, q_pos = [], []
+    for v in range(len(ln)):
+        c = min(rng.choice([0, 1, 1, 2, 4, 9]), ln[v] + 1)
+        q_node += [v] * c
+        q_pos += [ln[v] - c + i for i in range(c)]
+        if rng.random() < 0.2:
+            q_node.append(-1)
+            q_pos.append(rng.randint(-5, 5))
+    check(tree, q_node + [-1], q_pos + [0], rng.choice([1, 4, 8]), seed)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("G", [2, 8])
+def test_the_index_serves_growing_branches(kind, G):
+    ln = [777, 0, 10, 63, 100, 200]
+    tree = Tree([0, 6], [-1, 0, 0, 0, 0, 4], [0, 777, 777, 300, 777, 50], ln, 32, 2, kind, 5, grow=70)
+    q_node = [1, 2, 3, 4, 5, 5, 5]
+    q_pos = [-1, 9, 62, 99, 197, 198, 199]
+    for step in (0, 1, 2, 35, 70):
+        check(tree, q_node, q_pos, G, step, later=[p + step for p in q_pos])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_large_scores_and_far_apart_maxima(kind):
+    """Scores of some hundreds, growing along the sequence, so that the running maximum is raised again and again."""
+    tree = Tree([0, 1], [-1], [0], [2000], 64, 1, kind, 3)
+    grow = torch.linspace(0.01, 4, 2000, device="cuda").double()
+    at = tree.slots[0]
+    if kind == "bf16":
+        c = tree.cache[0]
+        c[at // 64, 0, at % 64] = (c[at // 64, 0, at % 64].double() * grow[:, None]).to(torch.bfloat16)
+        tree.values[0] = c.double()
+    check(tree, [0] * 3, [10, 1500, 1999], 8, 3, q_scale=8.0)
+
+
+@pytest.mark.parametrize("G", [1, 8, 16])
+def test_tokens_that_a_query_does_not_see_may_hold_anything(G):
+    """Drafts: later drafts' keys and values infinite or NaN; a fork: the parent's tokens behind it.  (All places of no node hold NaN already.)"""
+    tree = Tree([0, 3], [-1, 0, 0], [0, 100, 70], [131, 40, 9], 16, 1, "bf16", 4)
+    q_node, q_pos = [1, 1, 1, 2], [36, 37, 39, 8]
+    index = tree.index(q_node, q_pos, G)
+    q = queries(4, G, 4)
+    clean, clean_lse, _ = run(tree, index, q, q_pos, 0.1)
+    compare(clean, clean_lse, *tree.oracle(q, q_node, q_pos, 0.1))
+    for value in (float("nan"), float("inf"), float("-inf"), torch.finfo(torch.bfloat16).min):
+        for i in range(2):
+            at = torch.cat([tree.slots[1][38:40], tree.slots[0][100:]])
+            tree.cache[i][at // 16, 0, at % 16] = value
+        o, lse, status = run(tree, index, q, q_pos, 0.1)
+        H.harts_la_check(status)
+        for r in (0, 1, 3):
+            assert float((o[r].double() - clean[r].double()).norm()) <= 2.0 ** -8 * float(clean[r].double().norm()) and torch.equal(lse[r], clean_lse[r])
+
+
+def test_a_nan_that_is_seen_comes_out_as_one():
+    tree = Tree([0, 3], [-1, 0, 0], [0, 300, 300], [300, 40, 9], 16, 2, "bf16", 4)
+    s = tree.slots[0][5]
+    tree.cache[1][s // 16, 0, s % 16, 3] = float("nan")
+    s = tree.slots[1][7]
+    tree.cache[0][s // 16, 1, s % 16, 3] = float("nan")
+    index = tree.index([1, 2], [39, 8], 4)
+    o, lse, _ = run(tree, index, queries(2, 8, 4), [39, 8], 0.1)
+    want = torch.zeros(2, 8, 128, dtype=torch.bool, device="cuda")
+    want[:, :4, 3] = True                       # the value, seen by both
+    want[0, 4:] = True                          # the key, seen by the first
+    assert torch.equal(torch.isnan(o), want)
+    assert torch.equal(torch.isnan(lse), want.all(-1))
+
+
+def test_rows_of_nan_in_an_8_bit_cache():
+    tree = Tree([0, 3], [-1, 0, 0], [0, 300, 300], [300, 40, 9], 16, 2, "e4m3", 4)
+    s = tree.slots[1][7]
+    tree.exp[1][s // 16, 1, s % 16] = 255
+    index = tree.index([1, 2], [39, 8], 4)
+    o, lse, _ = run(tree, index, queries(2, 8, 4), [39, 8], 0.1)
+    want = torch.zeros(2, 8, 128, dtype=torch.bool, device="cuda")
+    want[0, 4:] = True
+    assert torch.equal(torch.isnan(o), want) and not torch.isnan(lse).any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_long_sequence_is_split(kind):
+    tree = Tree([0, 2], [-1, -1][:1] + [0], [0, 30000], [30000, 77], 64, 2, kind, 6)
+    index = check(tree, [1, 1], [75, 76], 4, 6)
+    assert index.n_narrow + index.n_wide > 20
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_captured_replayed_and_the_same_bits(kind):
+    ln = [900] + [50] * 40
+    tree = Tree([0, 41], [-1] + [0] * 40, [0] + [900] * 40, ln, 64, 2, kind, 7, grow=20)
+    q_node, q_pos = list(range(1, 41)), [49] * 40
+    index = tree.index(q_node, q_pos, 4)
+    q = queries(40, 8, 7)
+    ws = torch.full((index.workspace_bytes,), 255, dtype=torch.uint8, device="cuda")
+    o, lse, _ = run(tree, index, q, q_pos, 0.1, ws)
+    o2, lse2, pos = torch.empty_like(o), torch.empty_like(lse), torch.tensor(q_pos, dtype=torch.int32, device="cuda")
+    call = lambda: H.harts_gen_attn(index, q, *tree.cache, pos, o2, lse2, 0.1, workspace=ws, k_exp=tree.exp[0], v_exp=tree.exp[1])  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        o2.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    pos += 13                                             # the branches have grown
+    graph.replay()
+    torch.cuda.synchronize()
+    compare(o2, lse2, *tree.oracle(q, q_node, [62] * 40, 0.1))
+
+
+def test_positions_out_of_range_are_brought_in_and_reported():
+    ln = [500, 70, 130]
+    tree = Tree([0, 3], [-1, 0, 0], [0, 500, 500], ln, 32, 1, "bf16", 8, grow=10)
+    q_node, q_pos = [1, 2], [69, 129]
+    index = tree.index(q_node, q_pos, 4)
+    q = queries(2, 4, 8)
+    for r, bad, used in ((1, 140, 139), (0, 80, 79), (0, 2 ** 31 - 1, 79)):
+        pos = list(q_pos)
+        pos[r] = bad
+        o, lse, status = run(tree, index, q, pos, 0.1)
+        with pytest.raises(H.HartsError):
+            H.harts_la_check(status)
+        assert int(status[1]) == r
+        pos[r] = used
+        compare(o, lse, *tree.oracle(q, q_node, pos, 0.1))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_queries_of_a_wider_tensor_and_another_stream(kind):
+    tree = Tree([0, 3], [-1, 0, 0], [0, 300, 300], [300, 40, 9], 16, 2, kind, 9)
+    index = tree.index([1, 2], [39, 8], 4)
+    wide = torch.randn(2, 1024 + 256, device="cuda").to(torch.bfloat16)
+    q = wide[:, 128:128 + 1024].view(2, 8, 128)
+    a, la, _ = run(tree, index, q.contiguous(), [39, 8], 0.1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        b, lb, _ = run(tree, index, q, [39, 8], 0.1)
+    side.synchronize()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_nothing_to_see():
+    tree = Tree([0, 2], [-1, 0], [0, 0], [50, 0], 16, 1, "bf16", 10)
+    check(tree, [1, -1, 0], [-1, 7, 49], 4)
+    check(tree, [1], [-1], 4)
+    check(tree, [-1, -1], [3, 0], 4)
