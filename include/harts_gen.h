@@ -48,7 +48,7 @@ extern "C" {
  *   workspace: harts_gen_la_workspace_bytes(), for chunked calls only (NULL where that is 0).  Calls that share it, also as parts of
  *            captured graphs, must not run at the same time.
  * Served: fp32 with dk = dv = 64 or 128, bf16 with dk = dv = 64 or 128; chunks on the tensor cores for bf16 with 128, the others
- * walk token by token whatever their length.  States are fp32 and so are all sums; on the tensor cores the weighted keys are two bf16 terms each, so
+ * walk token by token whatever their length.  States are fp32 and so are all sums; on the tensor cores the weighted keys are three bf16 terms each, so
  * that states keep fp32's accuracy, while scores and the states that outputs are made of are rounded to bf16, as in harts_la.h.
  * A sequence with a bad entry is left out (dev_status[1] = its number).
  * Errors: HARTS_EINVAL (null or misaligned pointer, size out of range, workspace too small), HARTS_EUNSUPPORTED, HARTS_ECUDA.

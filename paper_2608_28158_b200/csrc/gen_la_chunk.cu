@@ -98,7 +98,7 @@ plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, in
 }
 
 // ---- sums of segments --------------------------------------------------------------------------------------------------------
-constexpr int PANEL = BT * 128, TILE = 2 * PANEL, STAGE = 3 * TILE, STAGES = 2, SUM_THREADS = 288, SUM_WARPS = 8;
+constexpr int PANEL = BT * 128, TILE = 2 * PANEL, STAGE = 2 * TILE, STAGES = 2, SUM_THREADS = 288, SUM_WARPS = 8;
 struct SumMisc {
     float w[MAX_L * BT];
     float warp_sum[SUM_WARPS];
@@ -106,7 +106,8 @@ struct SumMisc {
     uint32_t tmem;
     int dead;
 };
-constexpr int SUM_BYTES = STAGES * STAGE + sizeof(SumMisc) + 1024;
+// two stages of k, v, then the second and third terms of weighted keys
+constexpr int SUM_BYTES = STAGES * STAGE + 2 * TILE + sizeof(SumMisc) + 1024;
 
 __global__ void __launch_bounds__(SUM_THREADS, 2)
 sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const float* __restrict__ g, int H,
@@ -116,7 +117,7 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
     if (item >= *gen.count || !follows[item]) return;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    SumMisc& m = *reinterpret_cast<SumMisc*>(smem + STAGES * STAGE);
+    SumMisc& m = *reinterpret_cast<SumMisc*>(smem + STAGES * STAGE + 2 * TILE);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int4 it = gen.items[item];
     const int begin = it.x, len = it.y, n_chunks = len / BT;           // whole chunks: only a sequence's last segment may end inside one
@@ -159,10 +160,10 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
             const uint32_t tile = smem_u32(smem + st * STAGE);
             if (elect_one()) {
 #pragma unroll
-                for (int term = 0; term < 2; term++)
+                for (int term = 0; term < 3; term++)
 #pragma unroll
                     for (int ks = 0; ks < 4; ks++)
-                        mma_ss(tmem, desc_mnmajor<BT>(tile + term * 2 * TILE, ks), desc_mnmajor<BT>(tile + TILE, ks), IDESC, c > 0 || term > 0 || ks > 0);
+                        mma_ss(tmem, desc_mnmajor<BT>(term == 0 ? tile : smem_u32(smem) + STAGES * STAGE + (term - 1) * TILE, ks), desc_mnmajor<BT>(tile + TILE, ks), IDESC, c > 0 || term > 0 || ks > 0);
                 mma_commit(&m.done[st]);
             }
             __syncwarp();
@@ -203,23 +204,29 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         for (int c = 0; c < n_chunks; c++) {
             const int st = c % STAGES;
             if (!mbar_wait_warp(&m.full[st], (c / STAGES) & 1, status, &m.dead)) break;
-            unsigned char* tile = smem + st * STAGE;
+            // the tiles of second and third terms: the products before these are done
+            if (c > 0 && !mbar_wait_warp(&m.done[(c - 1) % STAGES], ((c - 1) / STAGES) & 1, status, &m.dead)) break;
+            unsigned char *tile = smem + st * STAGE, *rest = smem + STAGES * STAGE;
 #pragma unroll
             for (int u = 0; u < 4; u++) {
                 const int e = tid + u * 256, t = (e >> 3) & (BT - 1), off = (e >> 9) * PANEL + sw128_chunk(t, e & 7);
                 const float w = m.w[c * BT + t];
-                uint4 y = *reinterpret_cast<const uint4*>(tile + off), z;
-                auto terms = [&](uint32_t& x, uint32_t& rest) {
-                    const float p0 = __uint_as_float(x << 16) * w, p1 = __uint_as_float(x & 0xffff0000u) * w;
-                    x = pack_bf16(p0, p1);
-                    rest = pack_bf16(p0 - __uint_as_float(x << 16), p1 - __uint_as_float(x & 0xffff0000u));
+                uint4 y = *reinterpret_cast<const uint4*>(tile + off), z, z2;
+                auto terms = [&](uint32_t& t1, uint32_t& t2, uint32_t& t3) {
+                    float p0 = __uint_as_float(t1 << 16) * w, p1 = __uint_as_float(t1 & 0xffff0000u) * w;
+                    t1 = pack_bf16(p0, p1);
+                    p0 -= __uint_as_float(t1 << 16);
+                    p1 -= __uint_as_float(t1 & 0xffff0000u);
+                    t2 = pack_bf16(p0, p1);
+                    t3 = pack_bf16(p0 - __uint_as_float(t2 << 16), p1 - __uint_as_float(t2 & 0xffff0000u));
                 };
-                terms(y.x, z.x);
-                terms(y.y, z.y);
-                terms(y.z, z.z);
-                terms(y.w, z.w);
+                terms(y.x, z.x, z2.x);
+                terms(y.y, z.y, z2.y);
+                terms(y.z, z.z, z2.z);
+                terms(y.w, z.w, z2.w);
                 *reinterpret_cast<uint4*>(tile + off) = y;
-                *reinterpret_cast<uint4*>(tile + 2 * TILE + off) = z;
+                *reinterpret_cast<uint4*>(rest + off) = z;
+                *reinterpret_cast<uint4*>(rest + TILE + off) = z2;
             }
             fence_async_smem();
             __syncwarp();

@@ -18,8 +18,9 @@
 //
 // GEN: the same walk from and into kept states (harts_gen_la): the items come from a table that the call's first kernel has written, there
 // is neither replay nor a chunk-state workspace, and the state behind an item's last chunk is wanted.  It has to be as good as fp32 sums of
-// the given keys and values, so a weighted key is two bf16 terms, the second in a tile of its own, and K~^T V two products.  Rows
-// behind an item's end belong to others and may hold anything: a partial chunk's keys and values are zeroed there.
+// the given keys and values, so a weighted key is three bf16 terms (two leave 2.3e-6 of a state, three 1e-7), two of them in tiles of their
+// own, and K~^T V three products.  The room is that of the second tile of P, and masking has a barrier of its own, off the chain of sums.
+// Rows behind an item's end belong to others and may hold anything: a partial chunk's keys and values are zeroed there.
 //
 // What bounds it: HBM where chains are many (4,696 chunks x 32 heads 2,946 -> 2,480 us, 98 KB an item: 5.9 TB/s; 2,389 x 16 in chains of
 // up to 293 chunks 1,230 -> 700), else the 1.5 us of a chunk's busiest role (1,047 x 16 in 64 chains, two slices each: scan and chunk
@@ -62,7 +63,7 @@ struct Shape {
     static constexpr int OB = NV == 64 ? 2 : 1;            // output accumulators
     static constexpr int VP = NV / 64;                     // panels of 64 columns of v, the state and the outputs
     static constexpr int Q = 0, K = 2 * PANEL, V = 4 * PANEL, STAGE = V + VP * PANEL, S = VP * S_PANEL;
-    static constexpr int s = STAGES * STAGE, p = s + OUTS * S, lo = p + 2 * PANEL, misc = lo + (GEN ? 2 * PANEL : 0), bytes = misc + 9216 + 1024;
+    static constexpr int s = STAGES * STAGE, p = s + OUTS * S, lo = p + (GEN ? 1 : 2) * PANEL, misc = lo + (GEN ? 4 * PANEL : 0), bytes = misc + 9216 + 1024;
     // tensor memory: sums of a chunk (two), A (two), outputs (P V and Q S side by side)
     static constexpr int COL_U = 0, COL_A = 2 * NV, COL_O = COL_A + 128, COLS = 512;
     static_assert(COL_O + OB * 128 <= COLS, "tensor memory");
@@ -86,7 +87,7 @@ struct Record {              // one chunk
 struct Misc {
     Record rows[4];
     float raw[RAW][BT];
-    uint64_t full[4], stage_empty[4], a_full[2], ready[2], u_full[2], s_full[2], s_empty[2],
+    uint64_t full[4], stage_empty[4], a_full[2], ready[2], masked[2], u_full[2], s_full[2], s_empty[2],
         o_full[2], o_empty[2], gates_full[4], gates_empty[4], item_full[ITEMS], item_empty[ITEMS], exported[EXPORTS];
     Item items[ITEMS];
     uint32_t tmem;
@@ -151,12 +152,15 @@ __device__ __forceinline__ void mma_steps(uint32_t d, uint32_t a, uint32_t b, ui
     for (int ks = 1; ks < STEPS; ks++) mma_lo<true>(d, a + ks * SA + (ks >> 2) * GA, b + ks * SB + (ks >> 2) * GB, idesc);
 }
 
-// A weighted pair of keys, w k, as two terms of bf16.
-__device__ __forceinline__ void two_terms(uint32_t& x, uint32_t& rest, F2 w) {
+// A weighted pair of keys, w k, as three terms of bf16.
+__device__ __forceinline__ void three_terms(uint32_t& x, uint32_t& y, uint32_t& z, F2 w) {
     float a, b;
     f2_split(f2_mul(f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)), w), a, b);
     x = pack_bf16(a, b);
-    rest = pack_bf16(a - __uint_as_float(x << 16), b - __uint_as_float(x & 0xffff0000u));
+    a -= __uint_as_float(x << 16);
+    b -= __uint_as_float(x & 0xffff0000u);
+    y = pack_bf16(a, b);
+    z = pack_bf16(a - __uint_as_float(y << 16), b - __uint_as_float(y & 0xffff0000u));
 }
 
 template <int NV, bool GEN>
@@ -185,7 +189,8 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
         }
         for (int i = 0; i < 2; i++) {
             mbar_init(&m.a_full[i], 1);
-            mbar_init(&m.ready[i], NW / 32);
+            mbar_init(&m.ready[i], GEN ? NW / 64 : NW / 32);
+            mbar_init(&m.masked[i], NW / 64);
             mbar_init(&m.u_full[i], 1);
             mbar_init(&m.s_full[i], NS / 32);
             mbar_init(&m.s_empty[i], 2);                   // the product that read it, and the store warp
@@ -331,7 +336,8 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
         const int quarter = warp & 3, t = quarter * 32 + lane;
         const uint32_t tm_lane = tmem + ((uint32_t)(quarter * 32) << 16) + S::COL_A;
         Ring<STAGES> rg;
-        Ring<2> ra, rl;                           // rl: sums, the first of two terms each (GEN)
+        Ring<2> ra, rl;                           // GEN: rl, ro: the sum, the output of the chunk before (summed: there is one)
+        Ring<OB> ro;
         bool summed = false;
         uint32_t seen[16];                        // the diagonal's 32 columns, two to a register: ones where the row sees the column
 #pragma unroll
@@ -339,7 +345,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
         if (quarter == 0)                         // rows 0..31 see nothing of columns 32..63, in either tile of P
 #pragma unroll
             for (int u = 0; u < 8; u++)
-                *reinterpret_cast<uint4*>(smem + S::p + (u >> 2) * PANEL + sw128_chunk(t, 4 + (u & 3))) = make_uint4(0, 0, 0, 0);
+                if (!GEN || u < 4) *reinterpret_cast<uint4*>(smem + S::p + (u >> 2) * PANEL + sw128_chunk(t, 4 + (u & 3))) = make_uint4(0, 0, 0, 0);
         for (;;) {
             if (!wait(&m.gates_full[rg.i], rg.ph)) break;
             const Record& rd = m.rows[rg.i];
@@ -348,7 +354,14 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 // (behind A of this chunk: the product that read this tile of P two chunks ago, which was issued before it, is done too)
                 if (!wait(&m.a_full[ra.i], ra.ph)) break;
                 tc_fence_after();
-                unsigned char* sp = smem + S::p + ra.i * PANEL;
+                if constexpr (GEN) {              // one tile of P: the product that read the last one is done
+                    if (summed) {
+                        if (!wait(&m.o_full[ro.i], ro.ph)) break;
+                        ro.next();
+                    }
+                    summed = true;
+                }
+                unsigned char* sp = smem + S::p + (GEN ? 0 : ra.i) * PANEL;
                 uint32_t x[32];
                 tmem_ld32(tm_lane + ra.i * 64 + quarter * 32, x);
                 // the 32 columns on the diagonal
@@ -393,7 +406,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if constexpr (GEN) {
                     const int valid = rd.valid;
                     if (rd.step) {
-                        // the tile of second terms: the sum before this one has been made
+                        // the tiles of second and third terms: the sum before this one has been made
                         if (summed) {
                             if (!wait(&m.u_full[rl.i], rl.ph)) break;
                             rl.next();
@@ -412,14 +425,15 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                             }
 #pragma unroll
                             for (int u = 0; u < 4; u++) {
-                                uint4 z;
+                                uint4 z, z2;
                                 const F2 w2 = f2(w[u], w[u]);
-                                two_terms(y[u].x, z.x, w2);
-                                two_terms(y[u].y, z.y, w2);
-                                two_terms(y[u].z, z.z, w2);
-                                two_terms(y[u].w, z.w, w2);
+                                three_terms(y[u].x, z.x, z2.x, w2);
+                                three_terms(y[u].y, z.y, z2.y, w2);
+                                three_terms(y[u].z, z.z, z2.z, w2);
+                                three_terms(y[u].w, z.w, z2.w, w2);
                                 *reinterpret_cast<uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7)) = y[u];
                                 *reinterpret_cast<uint4*>(sl + sw128_chunk(t0 + 4 * u, lane & 7)) = z;
+                                *reinterpret_cast<uint4*>(sl + 2 * PANEL + sw128_chunk(t0 + 4 * u, lane & 7)) = z2;
                             }
                         }
                     }
@@ -452,7 +466,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
             }
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&m.ready[ra.i]);
+                mbar_arrive(GEN && quarter < 2 ? &m.masked[ra.i] : &m.ready[ra.i]);
                 mbar_arrive(&m.gates_empty[rg.i]);
             }
             rg.next();
@@ -674,7 +688,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                     if (elect_one()) {
                         mma_steps<4, MN, MN, 0, 0>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(tile + S::K), desc_lo_mn<BT>(tile + S::V), IDESC_U);
                         if constexpr (GEN)
-                            mma_steps<4, MN, MN, 0, 0, true>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(base + S::lo), desc_lo_mn<BT>(tile + S::V), IDESC_U);
+#pragma unroll
+                            for (int term = 0; term < 2; term++)
+                                mma_steps<4, MN, MN, 0, 0, true>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(base + S::lo + term * 2 * PANEL), desc_lo_mn<BT>(tile + S::V), IDESC_U);
                         mma_commit(&m.u_full[ru.i]);
                     }
                     __syncwarp();
@@ -686,10 +702,21 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if (elect_one()) {
                     mma_steps<8, MN, K, 0, KP>(acc + 64, desc_lo_mn<D>(base + S::s + rs.i * S::S), desc_lo_k(tile + S::Q), IDESC_O);
                     mma_commit(&m.s_empty[rs.i]);
-                    mma_steps<4, MN, K, 0, 0>(acc, desc_lo_mn<BT>(tile + S::V), desc_lo_k(base + S::p + rp.i * PANEL), IDESC_O);
-                    mma_commit(&m.o_full[rb.i]);
+                    if constexpr (!GEN) {
+                        mma_steps<4, MN, K, 0, 0>(acc, desc_lo_mn<BT>(tile + S::V), desc_lo_k(base + S::p + rp.i * PANEL), IDESC_O);
+                        mma_commit(&m.o_full[rb.i]);
+                    }
                 }
                 __syncwarp();
+                if constexpr (GEN) {
+                    if (!(alive = wait(&m.masked[rp.i], rp.ph))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        mma_steps<4, MN, K, 0, 0>(acc, desc_lo_mn<BT>(tile + S::V), desc_lo_k(base + S::p), IDESC_O);
+                        mma_commit(&m.o_full[rb.i]);
+                    }
+                    __syncwarp();
+                }
                 rt.next();
                 rs.next();
                 rb.next();
