@@ -4,14 +4,17 @@
 //     s_j = scale q . k_j    p_j = exp(s_j - m)    o = sum p_j v_j / sum p_j
 //
 // One CTA per (unit, key head): a warp asks for the pages by TMA, 64 tokens a stage; four warps take 16 of the 64 tokens each, so that every
-// key and value is read from shared memory once.  Products are m16n8k16 with the rows as m: at 16 rows a token the work is far below any
-// tensor path's rate, and its fragments let a warp keep scores, softmax and sums in registers.  A warp has its own running
-// maximum (raised in steps of 2^8 and more), sum and output; the four are joined at the unit's end.
-// 8-bit values become bf16 by moving bits and a multiplication by 2^120 (exact); which of the 128 elements a fragment's place
-// holds is free as long as both operands agree, so that a thread takes 32 bytes in a row of a key and 16 of a value.  A key's power of
-// two multiplies its score, a value's its p.
+// key and value is read from shared memory once.  Products are m16n8k16 with tokens (scores) and features (outputs) as m and the rows as n: 8
+// or 16 rows cost what they are, and fragments let a warp keep scores, softmax and sums in registers.  At so few rows a token the
+// work is far below any tensor path's rate.  A warp has its own running maximum (raised in steps of 2^8 and more), sum and output;
+// the four are joined at the unit's end.
+// 8-bit values become fp16 by one instruction a pair, exactly, so that the products are fp16 there: a row's queries times a power of two that
+// brings the largest to 2^14 (what falls below 2^-24 is 2^-38 of it), p with its token's power of two and a running maximum of
+// its own, and 11 bits of it kept instead of bf16's 8.  Which of the 128 features a fragment's place holds is free as long as both
+// operands agree, so that a thread takes 32 bytes in a row of a key and 16 of a value.
 // Bound by the cache's bytes.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "gen.h"
 #include "kernels.h"
@@ -37,35 +40,60 @@ struct Tables {
     const int32_t *pages, *part_ptr, *part;
     int n_q, Hq, Hkv, page;
 };
-template <bool F8>
+template <bool F8, int NR>             // NR: rows, in eights
 struct Shape {
-    static constexpr int KV = TILE * D * (F8 ? 1 : 2), EXP = F8 ? TILE : 0, STAGE = 2 * KV + 2 * EXP, STAGES = F8 ? 5 : 3;
+    // as many CTAs of an SM as registers allow, and stages for what shared memory is left
+    static constexpr int CTAS = NR == 1 ? (F8 ? 4 : 3) : 2, STAGES = NR == 1 ? (F8 ? 3 : 2) : (F8 ? 5 : 3);
+    static constexpr int KV = TILE * D * (F8 ? 1 : 2), EXP = F8 ? TILE : 0;
     // the exponents of a stage lie behind all tiles (which start on 1,024 bytes)
     static constexpr int exps = STAGES * 2 * KV, misc = exps + STAGES * 2 * EXP, bytes = misc + 256 + 1024;
     static constexpr int PITCH = D + 4;                       // floats of a row of O where the warps' parts are joined
-    static_assert(CW * NARROW_ROWS * (PITCH + 2) * 4 <= exps, "room for the parts");
+    static_assert(CW * 8 * NR * (PITCH + 4) * 4 <= exps, "room for the parts");
 };
 struct Misc {
     uint64_t full[5], empty[5];
     int dead;
 };
 
+template <bool F16>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void ldmatrix_x4(uint32_t saddr, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(saddr) : "memory");
 }
-// Two 8-bit values in the upper bytes of the halves of y, as bf16: sign | exponent and fraction four places down, times 2^120.
-__device__ __forceinline__ uint32_t widen(uint32_t y) {
-    const uint32_t x = ((y >> 4) & 0x07f007f0u) | (y & 0x80008000u);
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
-    return r;
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {      // an 8 x 8 matrix of 16-bit elements
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
-__device__ __forceinline__ bool nonfinite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+// two 8-bit values, the lower halves of x, as fp16
+__device__ __forceinline__ uint32_t widen(uint32_t x) {
+    uint32_t y;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t widen_upper(uint32_t x) {
+    uint32_t y;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <bool F8>             // whether any of the values is infinite or NaN (8 bits: 0x7f)
+__device__ __forceinline__ bool nonfinite(uint32_t x) {
+    if constexpr (F8) return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+    return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
 
 // Row i of a unit: its query and the query head; what it sees ends at `limit`.
 struct Row {
@@ -89,13 +117,14 @@ __device__ __forceinline__ Row row_of(const Tables& t, const Unit& u, int i, int
     return r;
 }
 
-template <bool F8>
-__global__ void __launch_bounds__(NT, 2)
+template <bool F8, int NR>
+__global__ void __launch_bounds__(NT, (Shape<F8, NR>::CTAS))
 narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, const __grid_constant__ CUtensorMap map_k,
               const __grid_constant__ CUtensorMap map_v, const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp,
               const int32_t* __restrict__ q_pos, float scale_log2, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ part_o,
               float* __restrict__ part_lse, int* status) {
-    using S = Shape<F8>;
+    using S = Shape<F8, NR>;
+    constexpr int ROWS = 8 * NR;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     Misc& m = *reinterpret_cast<Misc*>(smem + S::misc);
@@ -110,20 +139,12 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         m.dead = 0;
         fence_barrier_init();
     }
-    // rows g and g + 8 of this thread; the farthest token that any row sees, and the nearest limit
+    // what the unit's rows see: lane i has row i; the farthest token that any sees, and the nearest limit
     const int g = lane >> 2, c = lane & 3;
-    Row row[2];
-    int far = 0, near = INT32_MAX;
+    const Row mine = row_of(t, u, min(lane, ROWS - 1), h, q_pos, tid < ROWS ? status : nullptr);
+    int far = lane < u.n ? mine.limit : 0, near = lane < u.n ? mine.limit : INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        row[i] = row_of(t, u, g + 8 * i, h, q_pos, tid < 32 && c == 0 ? status : nullptr);
-        if (g + 8 * i < u.n) {
-            far = max(far, row[i].limit);
-            near = min(near, row[i].limit);
-        }
-    }
-#pragma unroll
-    for (int x = 4; x < 32; x <<= 1) {
+    for (int x = 1; x < 32; x <<= 1) {
         far = max(far, __shfl_xor_sync(~0u, far, x));
         near = min(near, __shfl_xor_sync(~0u, near, x));
     }
@@ -159,242 +180,278 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         }
         __syncwarp();
     } else {
-        uint32_t qa[8][4];                        // the rows' fragments
+        // ---- the rows' queries: n = row 8 r + g; scores of rows 8 r + 2 c, 8 r + 2 c + 1 -------------------------------------------------
+        uint32_t qb[NR][8][2];
+        float f[NR][2];                           // what makes a score log2 units
+        int limit[NR][2];
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const bool there = g + 8 * i < u.n;
-            const __nv_bfloat16* src = q + (int64_t)row[i].row * ld_q + (int64_t)row[i].head * D;
+        for (int r = 0; r < NR; r++) {
+            const int row = __shfl_sync(~0u, mine.row, 8 * r + g), head = __shfl_sync(~0u, mine.head, 8 * r + g);
+            const bool there = 8 * r + g < u.n;
+            const __nv_bfloat16* src = q + (int64_t)row * ld_q + (int64_t)head * D;
 #pragma unroll
             for (int ks = 0; ks < 8; ks++)
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
                     const int d = F8 ? 32 * c + 4 * ks + 2 * x : 16 * ks + 8 * x + 2 * c;
-                    qa[ks][2 * x + i] = there ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
+                    qb[r][ks][x] = there ? *reinterpret_cast<const uint32_t*>(src + d) : 0u;
                 }
-        }
-        float acc[16][4];
+            float own = scale_log2;
+            if constexpr (F8) {
+                uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 16; j++) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-        float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+                for (int ks = 0; ks < 8; ks++) top = __vmaxu2(top, __vmaxu2(qb[r][ks][0] & 0x7fff7fffu, qb[r][ks][1] & 0x7fff7fffu));
+                top = max(top & 0xffffu, top >> 16);
+                top = max(top, __shfl_xor_sync(~0u, top, 1));
+                top = max(top, __shfl_xor_sync(~0u, top, 2));
+                // 2^x with x = 14 less the largest exponent; zeros, infinities and NaN as they are.  Applied in two steps, as 2^x may be
+                // beyond fp32's largest power.
+                const int e = (int)(top >> 7), x = e == 0 || e == 255 ? 0 : 141 - e, x1 = x / 2;
+                const float f1 = __uint_as_float((uint32_t)(127 + x1) << 23), f2 = __uint_as_float((uint32_t)(127 + x - x1) << 23);
+#pragma unroll
+                for (int ks = 0; ks < 8; ks++)
+#pragma unroll
+                    for (int y = 0; y < 2; y++)
+                        qb[r][ks][y] = pack_f16(__uint_as_float(qb[r][ks][y] << 16) * f1 * f2, __uint_as_float(qb[r][ks][y] & 0xffff0000u) * f1 * f2);
+                own = scale_log2 * __uint_as_float((uint32_t)(127 - x1) << 23) * __uint_as_float((uint32_t)(127 - (x - x1)) << 23);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                f[r][y] = __shfl_sync(~0u, own, 4 * (2 * c + y));
+                limit[r][y] = __shfl_sync(~0u, mine.limit, 8 * r + 2 * c + y);         // (0 behind the unit's rows)
+            }
+        }
+        // top: of a score; top2: of a score and its value's power (8 bits), which p goes by
+        float acc[NR][8][4], top[NR][2], top2[NR][2], sum[NR][2];
+#pragma unroll
+        for (int r = 0; r < NR; r++) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) acc[r][j][0] = acc[r][j][1] = acc[r][j][2] = acc[r][j][3] = 0.f;
+            top[r][0] = top[r][1] = top2[r][0] = top2[r][1] = -INFINITY;
+            sum[r][0] = sum[r][1] = 0.f;
+        }
         for (int n = 0; n < n_tiles; n++) {
             const int st = n % S::STAGES, j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
             if (!mbar_wait_warp(&m.full[st], (n / S::STAGES) & 1, status, &m.dead)) break;
-            const unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV, *se = smem + S::exps + st * 2 * S::EXP;
-            float s[2][4] = {};
+            unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV;
+            const unsigned char* se = smem + S::exps + st * 2 * S::EXP + 16 * warp;
+            // scores of tokens g and g + 8
+            float s[NR][4];
+#pragma unroll
+            for (int r = 0; r < NR; r++) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
             if constexpr (F8) {
 #pragma unroll
-                for (int nt = 0; nt < 2; nt++) {
-                    const int key = 16 * warp + 8 * nt + g;
+                for (int x = 0; x < 2; x++) {
+                    const unsigned char* src = sk + sw128_chunk(16 * warp + g, 2 * c + x);
+                    const uint4 y = *reinterpret_cast<const uint4*>(src), z = *reinterpret_cast<const uint4*>(src + 8 * 128);
+                    const uint32_t w[4] = {y.x, y.y, y.z, y.w}, w8[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        const uint4 y = *reinterpret_cast<const uint4*>(sk + sw128_chunk(key, 2 * c + x));
-                        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t a[4] = {widen(w[i]), widen(w8[i]), widen_upper(w[i]), widen_upper(w8[i])};
 #pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            mma16816(s[nt], qa[4 * x + i], widen(__byte_perm(w[i], 0, 0x1404)), widen(__byte_perm(w[i], 0, 0x3424)));
+                        for (int r = 0; r < NR; r++) mma16816<true>(s[r], a, qb[r][4 * x + i][0], qb[r][4 * x + i][1]);
                     }
                 }
             } else {
 #pragma unroll
-                for (int k2 = 0; k2 < 4; k2++)
+                for (int ks = 0; ks < 8; ks++) {
+                    const int ch = 2 * ks + (lane >> 4);
+                    uint32_t a[4];
+                    ldmatrix_x4(smem_u32(sk) + (ch >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + (lane & 15), ch & 7), a);
 #pragma unroll
-                    for (int nt = 0; nt < 2; nt++) {
-                        const int key = 16 * warp + 8 * nt + (lane & 7), ch = 4 * k2 + (lane >> 3);
-                        uint32_t b[4];
-                        ldmatrix_x4(smem_u32(sk) + (ch >> 3) * (S::KV / 2) + sw128_chunk(key, ch & 7), b);
-                        mma16816(s[nt], qa[2 * k2], b[0], b[1]);
-                        mma16816(s[nt], qa[2 * k2 + 1], b[2], b[3]);
-                    }
-            }
-            // scores in log2 units; hidden tokens -inf
-            float vp[2][2];
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    float f = scale_log2;
-                    if constexpr (F8) {
-                        const int at = 16 * warp + 8 * nt + 2 * c + x;
-                        f *= gen_power(se[at]);
-                        vp[nt][x] = gen_power(se[TILE + at]);
-                    }
-                    s[nt][x] *= f;
-                    s[nt][2 + x] *= f;
+                    for (int r = 0; r < NR; r++) mma16816<false>(s[r], a, qb[r][ks][0], qb[r][ks][1]);
                 }
+            }
+            // in log2 units; hidden tokens -inf
             const bool edge = j0 < u.k0 || j0 + TILE > min(near, u.k1);
-            if (edge)
+            float kp[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f};
+            if constexpr (F8)
 #pragma unroll
-                for (int nt = 0; nt < 2; nt++)
+                for (int y = 0; y < 2; y++) {
+                    kp[y] = gen_power(se[g + 8 * y]);
+                    const int e = se[TILE + g + 8 * y];
+                    ve[y] = e == 255 ? __uint_as_float(0x7fffffffu) : (float)(e - 127);
+                }
+            uint32_t pb[NR][2];
+            bool any_raise = false;
+            float raise_by[NR][2];
+#pragma unroll
+            for (int r = 0; r < NR; r++) {
+                float mx[2], mx2[2];
+#pragma unroll
+                for (int x = 0; x < 4; x++) s[r][x] *= F8 ? f[r][x & 1] * kp[x >> 1] : f[r][x & 1];
+                if (edge)
 #pragma unroll
                     for (int x = 0; x < 4; x++) {
-                        const int key = key0 + 8 * nt + 2 * c + (x & 1);
-                        if (key < u.k0 || key >= min(row[x >> 1].limit, k1)) s[nt][x] = -INFINITY;
+                        const int key = key0 + g + 8 * (x >> 1);
+                        if (key < u.k0 || key >= min(limit[r][x & 1], k1)) s[r][x] = -INFINITY;
                     }
-            bool raise[2];
-            float mx[2];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                mx[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(~0u, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(~0u, mx[i], 2));
-                raise[i] = mx[i] > top[i] + RAISE || (top[i] == -INFINITY && mx[i] > -INFINITY);
-            }
-            if (__any_sync(~0u, raise[0] || raise[1])) {
-                float f[2];
+                for (int y = 0; y < 2; y++) {
+                    mx[y] = fmaxf(s[r][y], s[r][2 + y]);
+                    if constexpr (F8) mx2[y] = fmaxf(s[r][y] + ve[0], s[r][2 + y] + ve[1]);
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    f[i] = raise[i] ? ex2(top[i] - mx[i]) : 1.f;          // from -inf: 0, and all sums are 0
-                    if (raise[i]) top[i] = mx[i];
-                    sum[i] *= f[i];
-                }
-#pragma unroll
-                for (int j = 0; j < 16; j++) {
-                    acc[j][0] *= f[0];
-                    acc[j][1] *= f[0];
-                    acc[j][2] *= f[1];
-                    acc[j][3] *= f[1];
-                }
-            }
-            uint32_t pa[4];
-            const float base[2] = {top[0] == -INFINITY ? 0.f : top[0], top[1] == -INFINITY ? 0.f : top[1]};
-#pragma unroll
-            for (int nt = 0; nt < 2; nt++)
-#pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    float p0 = ex2(s[nt][2 * i] - base[i]), p1 = ex2(s[nt][2 * i + 1] - base[i]);
-                    sum[i] += p0 + p1;
-                    if constexpr (F8) {           // (a hidden token's power may be anything)
-                        p0 = p0 == 0.f ? 0.f : p0 * vp[nt][0];
-                        p1 = p1 == 0.f ? 0.f : p1 * vp[nt][1];
+                    for (int x = 4; x < 32; x <<= 1) {
+                        mx[y] = fmaxf(mx[y], __shfl_xor_sync(~0u, mx[y], x));
+                        if constexpr (F8) mx2[y] = fmaxf(mx2[y], __shfl_xor_sync(~0u, mx2[y], x));
                     }
-                    pa[2 * nt + i] = pack_bf16(p0, p1);
+                    if (mx[y] > top[r][y] + RAISE || (top[r][y] == -INFINITY && mx[y] > -INFINITY)) {
+                        const float by = ex2(top[r][y] - mx[y]);          // from -inf: 0, and all sums are 0
+                        sum[r][y] *= by;
+                        top[r][y] = mx[y];
+                        if constexpr (!F8) {
+                            raise_by[r][y] = by;
+                            any_raise = true;
+                        }
+                    } else if constexpr (!F8) {
+                        raise_by[r][y] = 1.f;
+                    }
+                    if constexpr (F8) {
+                        raise_by[r][y] = 1.f;
+                        if (mx2[y] > top2[r][y] + RAISE || (top2[r][y] == -INFINITY && mx2[y] > -INFINITY)) {
+                            raise_by[r][y] = ex2(top2[r][y] - mx2[y]);
+                            top2[r][y] = mx2[y];
+                            any_raise = true;
+                        }
+                    }
                 }
-            if constexpr (F8) {
+            }
+            if (__any_sync(~0u, any_raise)) {
+#pragma unroll
+                for (int r = 0; r < NR; r++)
+#pragma unroll
+                    for (int j = 0; j < 8; j++) {
+                        acc[r][j][0] *= raise_by[r][0];
+                        acc[r][j][1] *= raise_by[r][1];
+                        acc[r][j][2] *= raise_by[r][0];
+                        acc[r][j][3] *= raise_by[r][1];
+                    }
+            }
+#pragma unroll
+            for (int r = 0; r < NR; r++) {
+                float p[4];
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    const float base = top[r][y] == -INFINITY ? 0.f : top[r][y], base2 = top2[r][y] == -INFINITY ? 0.f : top2[r][y];
+#pragma unroll
+                    for (int x = y; x < 4; x += 2) {
+                        p[x] = ex2(s[r][x] - base);
+                        sum[r][y] += p[x];
+                        if constexpr (F8) p[x] = s[r][x] == -INFINITY ? 0.f : ex2(s[r][x] + ve[x >> 1] - base2);      // (a hidden token's power may be anything)
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < 2; x++) pb[r][x] = transposed(F8 ? pack_f16(p[2 * x], p[2 * x + 1]) : pack_bf16(p[2 * x], p[2 * x + 1]));
+            }
+            bool bad = false;
+            if (edge) {
+                // Behind the last token that any row sees: zeros (this warp's tokens; it is the last tile, nothing is loaded over them).
+                // Values that some rows see and others do not may be infinite or NaN, and 0 times that is not 0.
+                constexpr int CH = F8 ? 8 : 16;           // 16-byte pieces of a token's values
+#pragma unroll 1
+                for (int e = lane; e < 16 * CH; e += 32) {
+                    const int key = key0 + e / CH, ch = e % CH;
+                    if (key < k1 && key >= u.k0 && key < near) continue;
+                    uint4& y = *reinterpret_cast<uint4*>(sv + (ch >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + e / CH, ch & 7));
+                    if (key >= k1) y = make_uint4(0, 0, 0, 0);
+                    else bad |= nonfinite<F8>(y.x) || nonfinite<F8>(y.y) || nonfinite<F8>(y.z) || nonfinite<F8>(y.w);
+                }
+                bad = __any_sync(~0u, bad);
+                __syncwarp();
+            }
+            if (bad) {                             // token by token: what a row does not see adds nothing
+#pragma unroll 1
+                for (int key = 0; key < 16; key++)
+#pragma unroll
+                    for (int r = 0; r < NR; r++)
+#pragma unroll
+                        for (int y = 0; y < 2; y++) {
+                            // p of (token, row 8 r + 2 c + y): lane 4 (2 c + y) + (key / 2) % 4 has it
+                            const uint32_t w = __shfl_sync(~0u, key < 8 ? pb[r][0] : pb[r][1], 4 * (2 * c + y) + ((key & 7) >> 1)) >> (16 * (key & 1));
+                            const float p = F8 ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
+                            const bool sees = key0 + key >= u.k0 && key0 + key < min(limit[r][y], k1);
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+#pragma unroll
+                                for (int x = 0; x < 2; x++) {
+                                    const int d = F8 ? 16 * g + 2 * j + x : 16 * j + g + 8 * x;
+                                    float v;
+                                    if constexpr (F8) v = __half2float(__ushort_as_half((unsigned short)widen(sv[sw128_chunk(16 * warp + key, d >> 4) + (d & 15)])));
+                                    else v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(sv + (d >> 6) * (S::KV / 2) + sw128(16 * warp + key, d & 63)) << 16);
+                                    if (sees) acc[r][j][2 * x + y] += p * v;
+                                }
+                        }
+            } else if constexpr (F8) {
                 const unsigned char* v0 = sv + sw128_chunk(16 * warp + 2 * c, g);
                 const unsigned char* v1 = sv + sw128_chunk(16 * warp + 2 * c + 1, g);
                 const uint4 a = *reinterpret_cast<const uint4*>(v0), b = *reinterpret_cast<const uint4*>(v1);
                 const uint4 a8 = *reinterpret_cast<const uint4*>(v0 + 8 * 128), b8 = *reinterpret_cast<const uint4*>(v1 + 8 * 128);
                 const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w}, wa8[4] = {a8.x, a8.y, a8.z, a8.w}, wb8[4] = {b8.x, b8.y, b8.z, b8.w};
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    mma16816(acc[4 * i], pa, widen(__byte_perm(wa[i], wb[i], 0x4000)), widen(__byte_perm(wa8[i], wb8[i], 0x4000)));
-                    mma16816(acc[4 * i + 1], pa, widen(__byte_perm(wa[i], wb[i], 0x5010)), widen(__byte_perm(wa8[i], wb8[i], 0x5010)));
-                    mma16816(acc[4 * i + 2], pa, widen(__byte_perm(wa[i], wb[i], 0x6020)), widen(__byte_perm(wa8[i], wb8[i], 0x6020)));
-                    mma16816(acc[4 * i + 3], pa, widen(__byte_perm(wa[i], wb[i], 0x7030)), widen(__byte_perm(wa8[i], wb8[i], 0x7030)));
-                }
+                for (int i = 0; i < 4; i++)
+#pragma unroll
+                    for (int half = 0; half < 2; half++) {
+                        const uint32_t y = __byte_perm(wa[i], wb[i], half ? 0x7362 : 0x5140), y8 = __byte_perm(wa8[i], wb8[i], half ? 0x7362 : 0x5140);
+                        const uint32_t va[4] = {widen(y), widen_upper(y), widen(y8), widen_upper(y8)};
+#pragma unroll
+                        for (int r = 0; r < NR; r++) mma16816<true>(acc[r][2 * i + half], va, pb[r][0], pb[r][1]);
+                    }
             } else {
-                bool bad = false;
-                if (edge) {
-                    // Behind the last token that any row sees: zeros (this warp's tokens; it is the last tile, nothing is loaded over them).
-                    // Values that some rows see and others do not may be infinite or NaN, and 0 times that is not 0.
-                    if (key0 + 16 > k1) {
-#pragma unroll 1
-                        for (int e = lane + 16 * max(k1 - key0, 0); e < 256; e += 32)
-                            *reinterpret_cast<uint4*>(smem + st * 2 * S::KV + S::KV + ((e & 15) >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + (e >> 4), e & 7)) =
-                                make_uint4(0, 0, 0, 0);
-                        __syncwarp();
-                    }
 #pragma unroll
-                    for (int x = 0; x < 2; x++) {
-                        const int key = key0 + 2 * c + 8 * x;
-                        uint32_t any = 0;
-#pragma unroll 1
-                        for (int e = 0; e < 2; e++) {
-                            if (key + e >= k1 || (key + e >= u.k0 && key + e < near)) continue;
-#pragma unroll 1
-                            for (int ch = g; ch < 16; ch += 8) {
-                                const uint4 y = *reinterpret_cast<const uint4*>(sv + (ch >> 3) * (S::KV / 2) + sw128_chunk(key + e - j0, ch & 7));
-                                any |= nonfinite(y.x) || nonfinite(y.y) || nonfinite(y.z) || nonfinite(y.w);
-                            }
-                        }
-                        bad |= any != 0;
-                    }
-                    bad = __any_sync(~0u, bad);
-                }
-                if (!bad) {
+                for (int j = 0; j < 8; j++) {
+                    const int ch = 2 * j + ((lane >> 3) & 1);
+                    uint32_t va[4];
+                    ldmatrix_x4_trans(smem_u32(sv) + (ch >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + (lane & 7) + 8 * (lane >> 4), ch & 7), va);
 #pragma unroll
-                    for (int j2 = 0; j2 < 8; j2++) {
-                        const int key = 16 * warp + (lane & 15), ch = 2 * j2 + (lane >> 4);
-                        uint32_t b[4];
-                        ldmatrix_x4_trans(smem_u32(sv) + (ch >> 3) * (S::KV / 2) + sw128_chunk(key, ch & 7), b);
-                        mma16816(acc[2 * j2], pa, b[0], b[1]);
-                        mma16816(acc[2 * j2 + 1], pa, b[2], b[3]);
-                    }
-                } else {                           // row by row: what a row does not see adds nothing
-#pragma unroll 1
-                    for (int key = 0; key < 16; key++) {
-                        const int from = (lane & ~3) | ((key & 7) >> 1);
-                        float p[2];
-#pragma unroll
-                        for (int i = 0; i < 2; i++) {
-                            const uint32_t y = __shfl_sync(~0u, key < 8 ? pa[i] : pa[2 + i], from);
-                            p[i] = __uint_as_float((key & 1) ? y & 0xffff0000u : y << 16);
-                        }
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            const uint32_t y = *reinterpret_cast<const uint32_t*>(sv + (j >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + key, j & 7) + 4 * c);
-                            const float v0 = __uint_as_float(y << 16), v1 = __uint_as_float(y & 0xffff0000u);
-#pragma unroll
-                            for (int i = 0; i < 2; i++)
-                                if (key0 + key >= u.k0 && key0 + key < min(row[i].limit, k1)) {
-                                    acc[j][2 * i] += p[i] * v0;
-                                    acc[j][2 * i + 1] += p[i] * v1;
-                                }
-                        }
-                    }
+                    for (int r = 0; r < NR; r++) mma16816<false>(acc[r][j], va, pb[r][0], pb[r][1]);
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.empty[st]);
         }
         // ---- the four warps' parts joined -----------------------------------------------------------------------------------------
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            sum[i] += __shfl_xor_sync(~0u, sum[i], 1);
-            sum[i] += __shfl_xor_sync(~0u, sum[i], 2);
-        }
         float* so = reinterpret_cast<float*>(smem);
-        float* stats = so + CW * NARROW_ROWS * S::PITCH;                   // [warp][row]{maximum, sum}
+        float4* stats = reinterpret_cast<float4*>(so + CW * ROWS * S::PITCH);       // [warp][row]{maximum, sum, what outputs go by, -}
         asm volatile("bar.sync 1, 128;" ::: "memory");                   // all warps have read all stages
 #pragma unroll
-        for (int i = 0; i < 2; i++) {
-            float* dst = so + (warp * NARROW_ROWS + g + 8 * i) * S::PITCH;
+        for (int r = 0; r < NR; r++)
 #pragma unroll
-            for (int j = 0; j < 16; j++) {
-                if constexpr (F8) {
-                    dst[32 * c + j] = acc[j][2 * i];
-                    dst[32 * c + 16 + j] = acc[j][2 * i + 1];
-                } else {
-                    *reinterpret_cast<float2*>(dst + 8 * j + 2 * c) = make_float2(acc[j][2 * i], acc[j][2 * i + 1]);
-                }
+            for (int y = 0; y < 2; y++) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) sum[r][y] += __shfl_xor_sync(~0u, sum[r][y], x);
+                float* dst = so + (warp * ROWS + 8 * r + 2 * c + y) * S::PITCH;
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+#pragma unroll
+                    for (int x = 0; x < 2; x++) dst[F8 ? 16 * g + 2 * j + x : 16 * j + g + 8 * x] = acc[r][j][2 * x + y];
+                if (g == 0) stats[warp * ROWS + 8 * r + 2 * c + y] = make_float4(top[r][y], sum[r][y], F8 ? top2[r][y] : top[r][y], 0.f);
             }
-            if (c == 0) *reinterpret_cast<float2*>(stats + 2 * (warp * NARROW_ROWS + g + 8 * i)) = make_float2(top[i], sum[i]);
-        }
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        const int i = tid >> 3, e0 = (tid & 7) * 4;                       // row, and every 32nd element group of four
+        constexpr int PER = CW * 32 / ROWS;                               // threads a row
+        const int i = tid / PER;
+        const Row r = row_of(t, u, i, h, q_pos, nullptr);
         if (i < u.n) {
             float w[CW], M = -INFINITY, L = 0.f;
 #pragma unroll
-            for (int x = 0; x < CW; x++) M = fmaxf(M, stats[2 * (x * NARROW_ROWS + i)]);
+            for (int x = 0; x < CW; x++) M = fmaxf(M, stats[x * ROWS + i].x);
 #pragma unroll
             for (int x = 0; x < CW; x++) {
-                const float2 y = *reinterpret_cast<const float2*>(stats + 2 * (x * NARROW_ROWS + i));
-                w[x] = y.x == -INFINITY ? 0.f : ex2(y.x - M);
-                L += w[x] * y.y;
+                const float4 y = stats[x * ROWS + i];
+                L += y.x == -INFINITY ? 0.f * y.y : ex2(y.x - M) * y.y;
+                // a warp's output is in units of 2^top2; without a number there, though it has seen something: NaN
+                w[x] = y.y == 0.f ? 0.f : y.z == -INFINITY ? __uint_as_float(0x7fffffffu) : ex2(y.z - M);
             }
-            const bool none = M == -INFINITY && !(L != L);
+            const bool none = M == -INFINITY && L == 0.f;
             const float inv = none ? 0.f : 1.f / L;
-            const Row r = row_of(t, u, i, h, q_pos, nullptr);
             const int64_t out = (int64_t)r.row * t.Hq + r.head, part = (int64_t)(u.part0 + u.flat0 + i) * t.Hkv + h;
 #pragma unroll
-            for (int b = 0; b < 4; b++) {
-                const int e = e0 + 32 * b;
+            for (int e = tid % PER * 4; e < D; e += PER * 4) {
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (!none)
 #pragma unroll
                     for (int x = 0; x < CW; x++) {
                         if (w[x] == 0.f) continue;
-                        const float4 z = *reinterpret_cast<const float4*>(so + (x * NARROW_ROWS + i) * S::PITCH + e);
+                        const float4 z = *reinterpret_cast<const float4*>(so + (x * ROWS + i) * S::PITCH + e);
                         y.x += w[x] * z.x;
                         y.y += w[x] * z.y;
                         y.z += w[x] * z.z;
@@ -407,7 +464,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 if (r.alone) *reinterpret_cast<uint2*>(o + out * D + e) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
                 else *reinterpret_cast<float4*>(part_o + part * D + e) = y;
             }
-            if (e0 == 0) {
+            if (tid % PER == 0) {
                 const float l2 = none ? -INFINITY : M + log2f(L);
                 if (r.alone) lse[out] = l2 * LN2;
                 else part_lse[part] = l2;
@@ -461,12 +518,12 @@ merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __re
     if (lane == 0) lse[out] = M == -INFINITY && !nan ? -INFINITY : (M + log2f(L)) * LN2;
 }
 
-template <bool F8>
+template <bool F8, int NR>
 int32_t launch_narrow(const Tables& t, int n_units, const void* q, int64_t ld_q, const CUtensorMap& mk, const CUtensorMap& mv, const GenCache& c,
                       const int32_t* q_pos, void* o, float* lse, float scale, float* part_o, float* part_lse, int32_t* dev_status, cudaStream_t st) {
-    using S = Shape<F8>;
-    if (cudaFuncSetAttribute(narrow_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
-    narrow_kernel<F8><<<n_units * t.Hkv, NT, S::bytes, st>>>(t, (const __nv_bfloat16*)q, ld_q, mk, mv, c.k_exp, c.v_exp, q_pos, scale * LOG2E,
+    using S = Shape<F8, NR>;
+    if (cudaFuncSetAttribute(narrow_kernel<F8, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    narrow_kernel<F8, NR><<<n_units * t.Hkv, NT, S::bytes, st>>>(t, (const __nv_bfloat16*)q, ld_q, mk, mv, c.k_exp, c.v_exp, q_pos, scale * LOG2E,
                                                            (__nv_bfloat16*)o, lse, part_o, part_lse, dev_status);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
@@ -494,8 +551,8 @@ int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int
         const bool f8 = c.type == HARTS_E4M3;
         if ((rc = make_cache_map(&mk, c.k, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
         if ((rc = make_cache_map(&mv, c.v, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
-        rc = f8 ? launch_narrow<true>(t, hi[N_NARROW], q, ld_q, mk, mv, c, q_pos, o, lse, scale, part_o, part_lse, dev_status, st)
-                : launch_narrow<false>(t, hi[N_NARROW], q, ld_q, mk, mv, c, q_pos, o, lse, scale, part_o, part_lse, dev_status, st);
+        auto* narrow = hi[NARROW_MAX] <= 8 ? (f8 ? launch_narrow<true, 1> : launch_narrow<false, 1>) : (f8 ? launch_narrow<true, 2> : launch_narrow<false, 2>);
+        rc = narrow(t, hi[N_NARROW], q, ld_q, mk, mv, c, q_pos, o, lse, scale, part_o, part_lse, dev_status, st);
         if (rc != HARTS_OK) return rc;
     }
     if (hi[MERGED]) {

@@ -210,6 +210,7 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
         blob[MERGED] = ix.merged;
         blob[MAX_PAGE] = ix.max_page;
         blob[WORDS] = (int32_t)total;
+        for (const Unit& u : ix.narrow) blob[NARROW_MAX] = std::max(blob[NARROW_MAX], u.n);
         for (int i = 0; i < 6; i++) blob[NARROW + i] = (int32_t)at[i];
         auto put = [&](int i, const void* p, int64_t words) {
             if (words) std::copy_n(static_cast<const int32_t*>(p), words, blob + at[i]);

@@ -204,6 +204,28 @@ def test_large_scores_and_far_apart_maxima(kind):
     check(tree, [0] * 3, [10, 1500, 1999], 8, 3, q_scale=8.0)
 
 
+@pytest.mark.parametrize("G", [1, 4, 8])
+def test_tokens_that_a_query_does_not_see_may_hold_anything_8_bits(G):
+    """The same with NaN bytes, in places that no query sees and in later drafts, which see them."""
+    tree = Tree([0, 3], [-1, 0, 0], [0, 100, 70], [131, 40, 9], 16, 1, "e4m3", 4)
+    q_node, q_pos = [1, 1, 1, 2], [36, 37, 39, 8]
+    index = tree.index(q_node, q_pos, G)
+    q = queries(4, G, 4)
+    clean, clean_lse, _ = run(tree, index, q, q_pos, 0.1)
+    compare(clean, clean_lse, *tree.oracle(q, q_node, q_pos, 0.1))
+    used = torch.zeros(tree.cache[0].shape[0], 16, dtype=torch.bool, device="cuda")
+    for s in (tree.slots[0][:100], tree.slots[1][:38], tree.slots[2]):
+        used[s // 16, s % 16] = True
+    for i in range(2):
+        tree.cache[i].view(torch.uint8).transpose(1, 2)[~used] = 0x7f if i else 0xff
+        tree.exp[i].transpose(1, 2)[~used] = 254
+    o, lse, status = run(tree, index, q, q_pos, 0.1)
+    H.harts_la_check(status)
+    assert bool(torch.isnan(o[2]).all())
+    for r in (0, 1, 3):
+        assert float((o[r].double() - clean[r].double()).norm()) <= 2.0 ** -8 * float(clean[r].double().norm()) and torch.equal(lse[r], clean_lse[r])
+
+
 @pytest.mark.parametrize("G", [1, 8, 16])
 def test_tokens_that_a_query_does_not_see_may_hold_anything(G):
     """Drafts: later drafts' keys and values infinite or NaN; a fork: the parent's tokens behind it.  (All places of no node hold NaN already.)"""
@@ -320,3 +342,24 @@ def test_nothing_to_see():
     check(tree, [1, -1, 0], [-1, 7, 49], 4)
     check(tree, [1], [-1], 4)
     check(tree, [-1, -1], [3, 0], 4)
+
+
+@pytest.mark.parametrize("n", [1, 5, 40])
+def test_values_whose_powers_differ_much(n):
+    """8 bits: the value that a row attends to most may be 2^40 below its neighbours', and all of a sequence's may be tiny or NaN."""
+    tree = Tree([0, 1], [-1], [0], [n], 16, 1, "e4m3", 20 + n)
+    e = torch.randint(60, 190, tree.exp[1].shape, device="cuda").to(torch.uint8)
+    tree.exp[1].copy_(e)
+    tree.values[1] = tree.cache[1].float().double() * (e.cpu().double() - 127).exp2().cuda()[..., None]
+    check(tree, [0], [n - 1], 8, n, q_scale=30.0, scale=0.5)
+    tree.exp[1].fill_(255)
+    index = tree.index([0], [n - 1], 8)
+    o, lse, _ = run(tree, index, queries(1, 8, n), [n - 1], 0.1)
+    assert bool(torch.isnan(o).all()) and not bool(torch.isnan(lse).any())
+
+
+@pytest.mark.parametrize("scale", [1e-20, 1e-3, 1e4, 1e20])
+def test_queries_of_any_size(scale):
+    for kind in KINDS:
+        tree = Tree([0, 1], [-1], [0], [200], 32, 2, kind, 30)
+        check(tree, [0, 0], [150, 199], 4, 30, q_scale=scale, scale=0.1 / scale)
