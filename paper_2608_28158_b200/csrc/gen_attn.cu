@@ -13,33 +13,20 @@
 // its own, and 11 bits of it kept instead of bf16's 8.  Which of the 128 features a fragment's place holds is free as long as both
 // operands agree, so that a thread takes 32 bytes in a row of a key and 16 of a value.
 // Bound by the cache's bytes.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
+#include <algorithm>
 
-#include "gen.h"
+#include "gen_attn.cuh"
 #include "kernels.h"
-#include "tc_common.cuh"
 
 namespace harts {
-
-int32_t make_cache_map(CUtensorMap* map, const void* base, int64_t n, int32_t page, bool bytes);
-int sm_count();
 
 namespace {
 
 using namespace tc;
 using namespace gen_attn;
 
-constexpr int D = 128, TILE = 64, CW = 4, NT = CW * 32 + 32;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float RAISE = 8.f;
+constexpr int CW = 4, NT = CW * 32 + 32;
 
-struct Tables {
-    const Unit* units;
-    const Entry* entries;
-    const int32_t *pages, *part_ptr, *part;
-    int n_q, Hq, Hkv, page;
-};
 template <bool F8, int NR>             // NR: rows, in eights
 struct Shape {
     // as many CTAs of an SM as registers allow, and stages for what shared memory is left
@@ -74,47 +61,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {      // an 8 x 8 ma
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-// two 8-bit values, the lower halves of x, as fp16
-__device__ __forceinline__ uint32_t widen(uint32_t x) {
-    uint32_t y;
-    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t widen_upper(uint32_t x) {
-    uint32_t y;
-    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 template <bool F8>             // whether any of the values is infinite or NaN (8 bits: 0x7f)
 __device__ __forceinline__ bool nonfinite(uint32_t x) {
     if constexpr (F8) return __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
     return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-}
-
-// Row i of a unit: its query and the query head; what it sees ends at `limit`.
-struct Row {
-    int row, head, limit;
-    bool alone;                     // the query has no other part
-};
-__device__ __forceinline__ Row row_of(const Tables& t, const Unit& u, int i, int h, const int32_t* q_pos, int32_t* status) {
-    const int G = t.Hq / t.Hkv, flat = u.flat0 + min(i, u.n - 1);
-    const Entry e = t.entries[u.entry + flat / G];
-    Row r;
-    r.row = e.row;
-    r.head = h * G + flat % G;
-    r.alone = e.most < 0;
-    r.limit = e.limit;
-    if (e.limit < 0) {
-        const int most = e.most < 0 ? -e.most - 1 : e.most, pos = q_pos[e.row];
-        r.limit = pos < e.least ? (pos + 1 < e.least ? e.least : pos + 1) : pos >= most ? most : pos + 1;
-        if (status && (pos + 1 < e.least || pos >= most)) gen_report(status, e.row);
-    }
-    if (i >= u.n) r.limit = 0;
-    return r;
 }
 
 template <bool F8, int NR>
@@ -204,16 +154,12 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 top = max(top & 0xffffu, top >> 16);
                 top = max(top, __shfl_xor_sync(~0u, top, 1));
                 top = max(top, __shfl_xor_sync(~0u, top, 2));
-                // 2^x with x = 14 less the largest exponent; zeros, infinities and NaN as they are.  Applied in two steps, as 2^x may be
-                // beyond fp32's largest power.
-                const int e = (int)(top >> 7), x = e == 0 || e == 255 ? 0 : 141 - e, x1 = x / 2;
-                const float f1 = __uint_as_float((uint32_t)(127 + x1) << 23), f2 = __uint_as_float((uint32_t)(127 + x - x1) << 23);
+                const Fp16Scale x(top);
 #pragma unroll
                 for (int ks = 0; ks < 8; ks++)
 #pragma unroll
-                    for (int y = 0; y < 2; y++)
-                        qb[r][ks][y] = pack_f16(__uint_as_float(qb[r][ks][y] << 16) * f1 * f2, __uint_as_float(qb[r][ks][y] & 0xffff0000u) * f1 * f2);
-                own = scale_log2 * __uint_as_float((uint32_t)(127 - x1) << 23) * __uint_as_float((uint32_t)(127 - (x - x1)) << 23);
+                    for (int y = 0; y < 2; y++) qb[r][ks][y] = x.apply(qb[r][ks][y]);
+                own = x.undone(scale_log2);
             }
 #pragma unroll
             for (int y = 0; y < 2; y++) {
@@ -472,6 +418,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         }
     }
     if (__syncthreads_or(m.dead)) drain_delay();          // abandoned: copies in flight must land before the CTA goes
+    after_previous();                                     // (the wide kernel ran beside this one; the merge waits for this one only)
 }
 
 // A query head's parts joined: one warp each, four elements a lane.  Queries of one part have been written by their unit.
@@ -519,12 +466,16 @@ merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __re
 }
 
 template <bool F8, int NR>
-int32_t launch_narrow(const Tables& t, int n_units, const void* q, int64_t ld_q, const CUtensorMap& mk, const CUtensorMap& mv, const GenCache& c,
-                      const int32_t* q_pos, void* o, float* lse, float scale, float* part_o, float* part_lse, int32_t* dev_status, cudaStream_t st) {
+int32_t launch_narrow(const Tables& t, int n_units, const Call& a, bool follows) {
     using S = Shape<F8, NR>;
     if (cudaFuncSetAttribute(narrow_kernel<F8, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
-    narrow_kernel<F8, NR><<<n_units * t.Hkv, NT, S::bytes, st>>>(t, (const __nv_bfloat16*)q, ld_q, mk, mv, c.k_exp, c.v_exp, q_pos, scale * LOG2E,
-                                                           (__nv_bfloat16*)o, lse, part_o, part_lse, dev_status);
+    const auto *q = static_cast<const __nv_bfloat16*>(a.q);
+    auto* o = static_cast<__nv_bfloat16*>(a.o);
+    if (follows)
+        return launch_after(narrow_kernel<F8, NR>, n_units * t.Hkv, NT, S::bytes, a.stream, t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp,
+                            a.q_pos, a.scale_log2, o, a.lse, a.part_o, a.part_lse, a.dev_status) == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
+    narrow_kernel<F8, NR><<<n_units * t.Hkv, NT, S::bytes, a.stream>>>(t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp, a.q_pos, a.scale_log2, o,
+                                                                      a.lse, a.part_o, a.part_lse, a.dev_status);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
 
@@ -533,7 +484,6 @@ int32_t launch_narrow(const Tables& t, int n_units, const void* q, int64_t ld_q,
 int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int64_t ld_q, const GenCache& c, const int32_t* q_pos, void* o,
                  float* lse, float scale, void* workspace, int32_t* dev_status, cudaStream_t st) {
     Tables t;
-    t.units = reinterpret_cast<const Unit*>(di + hi[NARROW]);
     t.entries = reinterpret_cast<const Entry*>(di + hi[ENTRY]);
     t.pages = di + hi[PAGES];
     t.part_ptr = di + hi[PART_PTR];
@@ -544,16 +494,22 @@ int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int
     t.page = hi[PAGE];
     float* part_o = static_cast<float*>(workspace);
     float* part_lse = part_o + (size_t)hi[N_PARTS] * t.Hkv * D;
+    if ((int64_t)std::max(hi[N_NARROW], hi[N_WIDE]) * t.Hkv > INT32_MAX) return HARTS_EINVAL;
+    const bool f8 = c.type == HARTS_E4M3;
+    Call a{q, ld_q, {}, {}, c, q_pos, o, lse, part_o, part_lse, scale * LOG2E, dev_status, st};
+    int32_t rc;
+    if (hi[N_NARROW] > 0 || hi[N_WIDE] > 0) {
+        if ((rc = make_cache_map(&a.map_k, c.k, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
+        if ((rc = make_cache_map(&a.map_v, c.v, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
+    }
+    if (hi[N_WIDE] > 0) {
+        t.units = reinterpret_cast<const Unit*>(di + hi[WIDE]);
+        if ((rc = launch_wide(t, hi[N_WIDE], a)) != HARTS_OK) return rc;
+    }
     if (hi[N_NARROW] > 0) {
-        if ((int64_t)hi[N_NARROW] * t.Hkv > INT32_MAX) return HARTS_EINVAL;
-        CUtensorMap mk, mv;
-        int32_t rc;
-        const bool f8 = c.type == HARTS_E4M3;
-        if ((rc = make_cache_map(&mk, c.k, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
-        if ((rc = make_cache_map(&mv, c.v, (int64_t)c.n_pages * t.Hkv, t.page, f8)) != HARTS_OK) return rc;
+        t.units = reinterpret_cast<const Unit*>(di + hi[NARROW]);
         auto* narrow = hi[NARROW_MAX] <= 8 ? (f8 ? launch_narrow<true, 1> : launch_narrow<false, 1>) : (f8 ? launch_narrow<true, 2> : launch_narrow<false, 2>);
-        rc = narrow(t, hi[N_NARROW], q, ld_q, mk, mv, c, q_pos, o, lse, scale, part_o, part_lse, dev_status, st);
-        if (rc != HARTS_OK) return rc;
+        if ((rc = narrow(t, hi[N_NARROW], a, hi[N_WIDE] > 0)) != HARTS_OK) return rc;
     }
     if (hi[MERGED]) {
         const int64_t blocks = ((int64_t)t.n_q * t.Hq + MERGE_WARPS - 1) / MERGE_WARPS;

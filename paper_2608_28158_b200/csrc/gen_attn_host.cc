@@ -16,7 +16,6 @@ namespace {
 using namespace harts::gen_attn;
 
 constexpr int TILE = 64;
-constexpr bool HAVE_WIDE = false;
 constexpr int MIXED = 2 * TILE;         // limits this near to each other share a run
 constexpr int LEAST = 256;              // tokens a unit is not cut below
 constexpr int CTAS = 148 * 3;           // units wanted, all key heads together
@@ -68,7 +67,7 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
     std::vector<int32_t> parts_of(n_q, 0);
     auto add = [&](int node, int a, int b, bool wide, const std::vector<Entry>& e) {
         if (e.empty() || b <= a) return;
-        ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), HAVE_WIDE && wide && (int64_t)e.size() * G > NARROW_ROWS});
+        ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), wide && (int64_t)e.size() * G > NARROW_ROWS});
         ix.entries.insert(ix.entries.end(), e.begin(), e.end());
     };
     std::vector<Entry> e;

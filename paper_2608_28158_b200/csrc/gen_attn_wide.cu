@@ -1,0 +1,412 @@
+// Attention of sampled tokens on the cached tree: the wide kernel (up to 128 rows that read the same run of tokens) on tcgen05.
+//
+// One CTA per (unit, key head), in the roles of the training forward (attn_fwd.cu):
+//     S = Q K^T            tcgen05.mma, operands in shared memory, S in tensor memory (two tiles of 64 tokens)
+//     P = exp2(S - m)      four warps, one row per thread; P goes back to tensor memory as bf16 over S
+//     O += P V             tcgen05.mma with P as the tensor-memory operand
+// Pages come by TMA, a box of up to 64 tokens of one page each.  All rows see all tokens of the run; places of a tile ahead of it or behind it
+// are taken out of S, and their values (which may be anything) are zeroed, since 0 times an infinity is not 0.
+// 8 bits: pages land in a stage of their own, and four more warps make tiles of them -- keys fp16, by one instruction a pair (the
+// queries are brought to fp16 as in the narrow kernel), values bf16 by moving bits and a multiplication by 2^120, so that p times its
+// token's power of two needs no reference of its own.  Keys' powers multiply the scores.
+#include "gen_attn.cuh"
+#include "kernels.h"
+
+namespace harts {
+namespace gen_attn {
+namespace {
+
+using namespace tc;
+
+constexpr int NS = 128;                  // softmax threads, thread = row = tensor-memory lane
+template <bool F8>
+struct Shape {
+    static constexpr int NT = NS + 64 + (F8 ? 128 : 0);            // a warp that issues the MMAs, one that asks for pages, four that widen
+    static constexpr int CTAS = F8 ? 1 : 2;
+    static constexpr int Q_BYTES = WIDE_ROWS * D * 2, KV_BYTES = TILE * D * 2, RAW = F8 ? 2 * TILE * D : 0, RAW_EXP = F8 ? 2 * TILE : 0;
+    static constexpr int RAWS = F8 ? 3 : 0;                        // stages of pages
+    static constexpr int q = 0, k = Q_BYTES, v = k + 2 * KV_BYTES, raw = v + 2 * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
+    static constexpr int bytes = misc + 2560 + 1024;
+};
+constexpr int COL_S = 0, COL_O = 128, TMEM_COLS = 256;     // S / P of tile n at COL_S + 64 (n & 1)
+struct Misc {
+    float kp[2][TILE], vp[2][TILE];      // 8 bits: powers of a tile's tokens
+    float f[WIDE_ROWS];                  // what makes a row's score log2 units
+    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, raw[3], rawfree[3];
+    int dead;
+    uint32_t tmem;
+};
+static_assert(sizeof(Misc) <= 2560, "misc area");
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Two 8-bit values in the upper bytes of the halves of y, as bf16: sign | exponent and fraction four places down, times 2^120.
+__device__ __forceinline__ uint32_t widen_bf16(uint32_t y) {
+    const uint32_t x = ((y >> 4) & 0x07f007f0u) | (y & 0x80008000u);
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
+    return r;
+}
+
+template <bool F8>
+__global__ void __launch_bounds__(Shape<F8>::NT, Shape<F8>::CTAS)
+wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, const __grid_constant__ CUtensorMap map_k,
+            const __grid_constant__ CUtensorMap map_v, const uint8_t* __restrict__ k_exp, const uint8_t* __restrict__ v_exp,
+            const int32_t* __restrict__ q_pos, float scale_log2, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ part_o,
+            float* __restrict__ part_lse, int* status) {
+    using S = Shape<F8>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    Misc& m = *reinterpret_cast<Misc*>(smem + S::misc);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    let_next_launch();
+    const Unit u = t.units[blockIdx.x / t.Hkv];
+    const int h = blockIdx.x % t.Hkv;
+    const int tile0 = u.k0 & ~(TILE - 1), n_tiles = (u.k1 - tile0 + TILE - 1) / TILE;
+    if (tid == 0) {
+        for (int i = 0; i < 2; i++) {
+            mbar_init(&m.k[i], F8 ? 4 : 1);
+            mbar_init(&m.v[i], F8 ? 4 : 1);
+            mbar_init(&m.kfree[i], 1);
+            mbar_init(&m.vfree[i], 1);
+            mbar_init(&m.s[i], 1);
+            mbar_init(&m.p[i], NS / 32);
+        }
+        for (int i = 0; i < 3; i++) {
+            mbar_init(&m.raw[i], 1);
+            mbar_init(&m.rawfree[i], 4);
+        }
+        mbar_init(&m.pv, 1);
+        mbar_init(&m.o, 1);
+        mbar_init(&m.exit, 1);
+        m.dead = 0;
+        fence_barrier_init();
+    }
+    if (warp == 0) tmem_alloc<TMEM_COLS>(&m.tmem);
+    // the rows' queries, half a warp a row
+    for (int i = tid >> 4; i < WIDE_ROWS; i += S::NT / 16) {
+        const int ch = tid & 15;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (i < u.n) {
+            const int G = t.Hq / t.Hkv, flat = u.flat0 + i;
+            x = *reinterpret_cast<const uint4*>(q + (int64_t)t.entries[u.entry + flat / G].row * ld_q + (int64_t)(h * G + flat % G) * D + ch * 8);
+        }
+        if constexpr (F8) {
+            uint32_t w[4] = {x.x, x.y, x.z, x.w}, top = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
+            top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+            const Fp16Scale f(top);
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = f.apply(w[e]);
+            x = make_uint4(w[0], w[1], w[2], w[3]);
+            if (ch == 0) m.f[i] = f.undone(scale_log2);
+        }
+        *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
+    }
+    fence_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = m.tmem;
+
+    if (warp == NS / 32 + 1) {
+        // ---- pages ---------------------------------------------------------------------------------------------------------------------
+        if (lane == 0) {
+            const int box = min(t.page, TILE), box_shift = 31 - __clz(box), page_shift = 31 - __clz(t.page);
+            for (int n = 0; n < n_tiles; n++) {
+                const int st = n & 1, rs = n % 3;
+                const int j0 = tile0 + n * TILE, boxes = (min(u.k1 - j0, TILE) + box - 1) >> box_shift;
+                auto block_of = [&](int j) { return (int64_t)t.pages[u.page0 + (j >> page_shift)] * t.Hkv + h; };
+                if constexpr (F8) {
+                    unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
+                    if (!mbar_wait(&m.rawfree[rs], ((n / 3) & 1) ^ 1, status, &m.dead)) break;
+                    mbar_expect_tx(&m.raw[rs], boxes * box * (2 * D + 2));
+                    for (int b = 0; b < boxes; b++) {
+                        const int j = j0 + (b << box_shift), at = j & (t.page - 1);
+                        const int64_t block = block_of(j);
+                        tma_load_3d(raw + b * box * D, &map_k, 0, at, (int)block, &m.raw[rs]);
+                        tma_load_3d(raw + TILE * D + b * box * D, &map_v, 0, at, (int)block, &m.raw[rs]);
+                        bulk_load(exps + b * box, k_exp + block * t.page + at, box, &m.raw[rs]);
+                        bulk_load(exps + TILE + b * box, v_exp + block * t.page + at, box, &m.raw[rs]);
+                    }
+                } else {
+                    unsigned char *sk = smem + S::k + st * S::KV_BYTES, *sv = smem + S::v + st * S::KV_BYTES;
+                    if (!mbar_wait(&m.kfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+                    mbar_expect_tx(&m.k[st], boxes * box * 2 * D);
+                    for (int b = 0; b < boxes; b++) {
+                        const int j = j0 + (b << box_shift);
+                        for (int p = 0; p < 2; p++)
+                            tma_load_3d(sk + p * (S::KV_BYTES / 2) + b * box * 128, &map_k, p * 64, j & (t.page - 1), (int)block_of(j), &m.k[st]);
+                    }
+                    if (!mbar_wait(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+                    mbar_expect_tx(&m.v[st], boxes * box * 2 * D);
+                    for (int b = 0; b < boxes; b++) {
+                        const int j = j0 + (b << box_shift);
+                        for (int p = 0; p < 2; p++)
+                            tma_load_3d(sv + p * (S::KV_BYTES / 2) + b * box * 128, &map_v, p * 64, j & (t.page - 1), (int)block_of(j), &m.v[st]);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == NS / 32) {
+        // ---- MMA issue: S as wide as the tile has tokens (steps of 16), P V as deep -----------------------------------------------------------
+        constexpr uint32_t I_O = instr_desc(WIDE_ROWS, D, 0, 1);
+        const uint64_t dQ = desc_kmajor_base(smem_u32(smem + S::q));
+        auto valid = [&](int n) { return min(u.k1 - tile0 - n * TILE, TILE); };
+        auto issue_s = [&](int n) {
+            const int st = n & 1;
+            if (!mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) return false;
+            tc_fence_after();
+            const uint32_t idesc = F8 ? instr_desc_f16(WIDE_ROWS, (valid(n) + 15) & ~15) : instr_desc(WIDE_ROWS, (valid(n) + 15) & ~15, 0, 0);
+            const uint64_t dK = desc_kmajor_base(smem_u32(smem + S::k + st * S::KV_BYTES));
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < 8; ks++) mma_ss(tmem + COL_S + st * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks), dK + kstep_kmajor<TILE>(ks), idesc, ks > 0);
+                mma_commit(&m.s[st]);
+                mma_commit(&m.kfree[st]);
+            }
+            __syncwarp();
+            return true;
+        };
+        bool alive = issue_s(0);
+        for (int n = 0; n < n_tiles && alive; n++) {
+            const int st = n & 1, steps = (valid(n) + 15) >> 4;
+            // S of tile n + 1 goes to the other buffer and runs under the softmax of tile n (that buffer's P was read by the P V
+            // MMAs of tile n - 1, which precede it in the pipe)
+            if (n + 1 < n_tiles && !(alive = issue_s(n + 1))) break;
+            if (!(alive = mbar_wait_warp(&m.v[st], (n >> 1) & 1, status, &m.dead))) break;
+            if (!F8 && (valid(n) < steps * 16 || (n == 0 && tile0 < u.k0))) {      // (8 bits: zeroed where they are widened)
+                unsigned char* sv = smem + S::v + st * S::KV_BYTES;
+                for (int e = lane; e < TILE * 16; e += 32) {
+                    const int key = e >> 4, ch = e & 15;
+                    if (tile0 + n * TILE + key < u.k0 || key >= valid(n))
+                        *reinterpret_cast<uint4*>(sv + (ch >> 3) * (S::KV_BYTES / 2) + sw128_chunk(key, ch & 7)) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_smem();
+                __syncwarp();
+            }
+            if (!(alive = mbar_wait_warp(&m.p[st], (n >> 1) & 1, status, &m.dead))) break;
+            tc_fence_after();
+            const uint64_t dV = desc_mnmajor_base<TILE>(smem_u32(smem + S::v + st * S::KV_BYTES));
+            if (elect_one()) {
+#pragma unroll 1
+                for (int ks = 0; ks < steps; ks++)
+                    mma_ts(tmem + COL_O, tmem + COL_S + st * 64 + ks * 8, dV + kstep_mnmajor(ks), I_O, n > 0 || ks > 0);
+                mma_commit(&m.pv);                                    // one phase per tile, in order
+                mma_commit(&m.vfree[st]);
+                if (n + 1 == n_tiles) mma_commit(&m.o);
+            }
+            __syncwarp();
+        }
+    } else if (F8 && warp >= NS / 32 + 2) {
+        // ---- 8-bit pages -> tiles ---------------------------------------------------------------------------------------------------------
+        const int wt = tid - NS - 64;
+        for (int n = 0; n < n_tiles; n++) {
+            const int st = n & 1, rs = n % 3, j0 = tile0 + n * TILE;
+            if (!mbar_wait_warp(&m.raw[rs], (n / 3) & 1, status, &m.dead)) break;
+            // the powers' places are free when P of two tiles ago has been used
+            if (!mbar_wait_warp(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+            if (!mbar_wait_warp(&m.kfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+            const unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
+            unsigned char *sk = smem + S::k + st * S::KV_BYTES, *sv = smem + S::v + st * S::KV_BYTES;
+            if (wt < TILE) m.kp[st][wt] = gen_power(exps[wt]);
+            else m.vp[st][wt - TILE] = gen_power(exps[wt]);
+#pragma unroll
+            for (int x = 0; x < 4; x++) {                             // 16 features of a key each
+                const int e = wt + 128 * x, key = e >> 3, ch = e & 7;
+                const uint4 y = *reinterpret_cast<const uint4*>(raw + sw128_chunk(key, ch));
+                unsigned char* dst = sk + (ch >> 2) * (S::KV_BYTES / 2);
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch) & 7)) = make_uint4(widen(y.x), widen_upper(y.x), widen(y.y), widen_upper(y.y));
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch + 1) & 7)) = make_uint4(widen(y.z), widen_upper(y.z), widen(y.w), widen_upper(y.w));
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.k[st]);
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                const int e = wt + 128 * x, key = e >> 3, ch = e & 7;
+                uint4 y = *reinterpret_cast<const uint4*>(raw + TILE * D + sw128_chunk(key, ch));
+                if (j0 + key < u.k0 || j0 + key >= u.k1) y = make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                uint32_t z[8];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    z[2 * i] = widen_bf16(__byte_perm(w[i], 0, 0x1404));
+                    z[2 * i + 1] = widen_bf16(__byte_perm(w[i], 0, 0x3424));
+                    if (__vcmpeq4(w[i] & 0x7f7f7f7fu, 0x7f7f7f7fu)) {          // a NaN byte
+                        auto nan_or = [&](uint32_t v, int b) {
+                            return v | ((w[i] >> b & 0x7fu) == 0x7fu ? 0x7fffu : 0u) | ((w[i] >> (b + 8) & 0x7fu) == 0x7fu ? 0x7fff0000u : 0u);
+                        };
+                        z[2 * i] = nan_or(z[2 * i], 0);
+                        z[2 * i + 1] = nan_or(z[2 * i + 1], 16);
+                    }
+                }
+                unsigned char* dst = sv + (ch >> 2) * (S::KV_BYTES / 2);
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch) & 7)) = make_uint4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch + 1) & 7)) = make_uint4(z[4], z[5], z[6], z[7]);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&m.v[st]);
+                mbar_arrive(&m.rawfree[rs]);
+            }
+        }
+    } else {
+        // ---- softmax: a row per thread -----------------------------------------------------------------------------------------------------
+        const uint32_t tm_lane = tmem + ((uint32_t)(warp * 32) << 16);
+        const float f = F8 ? m.f[tid] : scale_log2;
+        const F2 f2v = f2(f, f);
+        float m_ref = -INFINITY, l_sum = 0.f;
+        for (int n = 0; n < n_tiles; n++) {
+            const int st = n & 1, j0 = tile0 + n * TILE;
+            if (!mbar_wait_warp(&m.s[st], (n >> 1) & 1, status, &m.dead)) break;
+            if (F8 && !mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) break;        // (complete: orders the powers)
+            tc_fence_after();
+            uint32_t x[TILE];
+            tmem_ld32(tm_lane + COL_S + st * 64, x);
+            tmem_ld32(tm_lane + COL_S + st * 64 + 32, x + 32);
+            tmem_ld_wait();
+            if constexpr (F8) {
+#pragma unroll
+                for (int e = 0; e < TILE; e += 4) {
+                    const float4 kp = *reinterpret_cast<const float4*>(&m.kp[st][e]);
+                    float a, b;
+                    f2_split(f2_mul(f2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), f2(kp.x, kp.y)), a, b);
+                    x[e] = __float_as_uint(a);
+                    x[e + 1] = __float_as_uint(b);
+                    f2_split(f2_mul(f2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), f2(kp.z, kp.w)), a, b);
+                    x[e + 2] = __float_as_uint(a);
+                    x[e + 3] = __float_as_uint(b);
+                }
+            }
+            if (j0 < u.k0 || j0 + TILE > u.k1) {
+#pragma unroll
+                for (int e = 0; e < TILE; e++)
+                    if (j0 + e < u.k0 || j0 + e >= u.k1) x[e] = __float_as_uint(-INFINITY);
+            }
+            float mx = __uint_as_float(x[0]);
+#pragma unroll
+            for (int e = 1; e + 1 < TILE; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+            mx = fmaxf(mx, __uint_as_float(x[TILE - 1])) * f;
+            const bool raise = mx > m_ref + RAISE || (m_ref == -INFINITY && mx > -INFINITY);
+            if (__any_sync(~0u, raise && n > 0)) {
+                // O is about to be read and rewritten: the P V MMAs of the tile before must be done (this warp is never more than a phase behind)
+                if (!mbar_wait_warp(&m.pv, (n - 1) & 1, status, &m.dead)) break;
+                tc_fence_after();
+                const float m_new = raise ? mx : m_ref;
+                const float alpha = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
+                l_sum *= alpha;
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    uint32_t y[32];
+                    tmem_ld32(tm_lane + COL_O + c * 32, y);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+                    tmem_st32(tm_lane + COL_O + c * 32, y);
+                }
+                m_ref = m_new;
+            } else if (raise) {
+                m_ref = mx;                               // first tile: nothing accumulated yet
+            }
+            const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
+            const F2 nm = f2(neg_m, neg_m);
+            F2 part[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    float p0, p1;
+                    f2_split(f2_fma(f2(__uint_as_float(x[c * 32 + e]), __uint_as_float(x[c * 32 + e + 1])), f2v, nm), p0, p1);
+                    p0 = ex2(p0);
+                    p1 = ex2(p1);
+                    part[(e >> 1) & 1] = f2_add(part[(e >> 1) & 1], f2(p0, p1));
+                    if constexpr (F8) {
+                        const float2 vp = *reinterpret_cast<const float2*>(&m.vp[st][c * 32 + e]);
+                        p0 = p0 == 0.f ? 0.f : p0 * vp.x;             // (behind the run a power may be anything)
+                        p1 = p1 == 0.f ? 0.f : p1 * vp.y;
+                    }
+                    pk[e >> 1] = pack_bf16(p0, p1);
+                }
+                tmem_st16(tm_lane + COL_S + st * 64 + c * 16, pk);
+            }
+            float a0, a1;
+            f2_split(f2_add(part[0], part[1]), a0, a1);
+            l_sum += a0 + a1;
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.p[st]);
+        }
+        // ---- O / l, and its place -----------------------------------------------------------------------------------------------------------
+        const bool ok = mbar_wait_warp(&m.o, 0, status, &m.dead);
+        tc_fence_after();
+        const bool mine = ok && tid < u.n;
+        const Row r = row_of(t, u, tid, h, q_pos, nullptr);
+        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
+        const int64_t out = (int64_t)r.row * t.Hq + r.head, part = (int64_t)(u.part0 + u.flat0 + tid) * t.Hkv + h;
+        if (mine) {
+            const float l2 = m_ref + log2f(l_sum);
+            if (r.alone) lse[out] = l2 * LN2;
+            else part_lse[part] = l2;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            uint32_t x[32];
+            tmem_ld32(tm_lane + COL_O + c * 32, x);
+            tmem_ld_wait();
+            if (!mine) continue;
+#pragma unroll
+            for (int e = 0; e < 32; e++) x[e] = __float_as_uint(__uint_as_float(x[e]) * inv);
+            if (r.alone) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8)
+                    *reinterpret_cast<uint4*>(o + out * D + c * 32 + e) =
+                        make_uint4(pack_bf16(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pack_bf16(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])),
+                                   pack_bf16(__uint_as_float(x[e + 4]), __uint_as_float(x[e + 5])), pack_bf16(__uint_as_float(x[e + 6]), __uint_as_float(x[e + 7])));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part_o + part * D + c * 32 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+            }
+        }
+    }
+    __syncwarp();
+    if (__syncthreads_or(m.dead)) {               // abandoned: let the loads and MMAs in flight finish (bounded)
+        if (warp == NS / 32 && elect_one()) {
+            mma_commit(&m.exit);
+            mbar_wait_drain(&m.exit, 0);
+        }
+        drain_delay();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc<TMEM_COLS>(tmem);
+}
+
+template <bool F8>
+int32_t launch(const Tables& t, int n_units, const Call& a) {
+    using S = Shape<F8>;
+    if (cudaFuncSetAttribute(wide_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    wide_kernel<F8><<<n_units * t.Hkv, S::NT, S::bytes, a.stream>>>(t, static_cast<const __nv_bfloat16*>(a.q), a.ld_q, a.map_k, a.map_v, a.cache.k_exp,
+                                                                  a.cache.v_exp, a.q_pos, a.scale_log2, static_cast<__nv_bfloat16*>(a.o), a.lse, a.part_o,
+                                                                  a.part_lse, a.dev_status);
+    return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
+}
+
+}  // namespace
+
+int32_t launch_wide(const Tables& t, int n_units, const Call& a) {
+    return a.cache.type == HARTS_E4M3 ? launch<true>(t, n_units, a) : launch<false>(t, n_units, a);
+}
+
+}  // namespace gen_attn
+}  // namespace harts
