@@ -103,32 +103,31 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
 
     if (warp == CW) {
         // ---- pages: a box is up to 64 tokens of one page ----------------------------------------------------------------------------
-        if (lane == 0) {
-            const int box = min(t.page, TILE), box_shift = 31 - __clz(box), page_shift = 31 - __clz(t.page);
-            for (int n = 0; n < n_tiles; n++) {
-                const int st = n % S::STAGES;
-                if (!mbar_wait(&m.empty[st], ((n / S::STAGES) & 1) ^ 1, status, &m.dead)) break;
-                const int j0 = tile0 + n * TILE, boxes = (min(k1 - j0, TILE) + box - 1) >> box_shift;
-                unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV, *se = smem + S::exps + st * 2 * S::EXP;
-                mbar_expect_tx(&m.full[st], boxes * box * (F8 ? 2 * D + 2 : 4 * D));
-                for (int b = 0; b < boxes; b++) {
-                    const int j = j0 + (b << box_shift), at = j & (t.page - 1);
-                    const int64_t block = (int64_t)t.pages[u.page0 + (j >> page_shift)] * t.Hkv + h;
-                    if constexpr (F8) {
-                        tma_load_3d(sk + b * box * D, &map_k, 0, at, (int)block, &m.full[st]);
-                        tma_load_3d(sv + b * box * D, &map_v, 0, at, (int)block, &m.full[st]);
-                        bulk_load(se + b * box, k_exp + block * t.page + at, box, &m.full[st]);
-                        bulk_load(se + TILE + b * box, v_exp + block * t.page + at, box, &m.full[st]);
-                    } else {
-                        for (int p = 0; p < 2; p++) {
-                            tma_load_3d(sk + p * (S::KV / 2) + b * box * 128, &map_k, p * 64, at, (int)block, &m.full[st]);
-                            tma_load_3d(sv + p * (S::KV / 2) + b * box * 128, &map_v, p * 64, at, (int)block, &m.full[st]);
-                        }
+        PageWalk walk(t, u, tile0, k1);
+        const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
+        for (int n = 0; n < n_tiles; n++) {
+            const int st = n % S::STAGES;
+            if (!mbar_wait_warp(&m.empty[st], ((n / S::STAGES) & 1) ^ 1, status, &m.dead)) break;
+            const int j0 = tile0 + n * TILE, boxes = (min(k1 - j0, TILE) + box - 1) >> walk.box_shift;
+            unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV, *se = smem + S::exps + st * 2 * S::EXP;
+            if (lane == 0) mbar_expect_tx(&m.full[st], boxes * box * (F8 ? 2 * D + 2 : 4 * D));
+            for (int b = 0; b < boxes; b++) {
+                const int at = (j0 + (b << walk.box_shift)) & (t.page - 1), block = walk.of(n * per_tile + b) * t.Hkv + h;
+                if (lane != 0) continue;
+                if constexpr (F8) {
+                    tma_load_3d(sk + b * box * D, &map_k, 0, at, block, &m.full[st]);
+                    tma_load_3d(sv + b * box * D, &map_v, 0, at, block, &m.full[st]);
+                    bulk_load(se + b * box, k_exp + (int64_t)block * t.page + at, box, &m.full[st]);
+                    bulk_load(se + TILE + b * box, v_exp + (int64_t)block * t.page + at, box, &m.full[st]);
+                } else {
+                    for (int p = 0; p < 2; p++) {
+                        tma_load_3d(sk + p * (S::KV / 2) + b * box * 128, &map_k, p * 64, at, block, &m.full[st]);
+                        tma_load_3d(sv + p * (S::KV / 2) + b * box * 128, &map_v, p * 64, at, block, &m.full[st]);
                     }
                 }
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else {
         // ---- the rows' queries: n = row 8 r + g; scores of rows 8 r + 2 c, 8 r + 2 c + 1 -------------------------------------------------
         uint32_t qb[NR][8][2];

@@ -60,6 +60,30 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// The pages of a unit's boxes (up to 64 tokens of one page), asked for 32 at a time by a whole warp and a batch ahead of their use: a load for
+// each box, by the thread that has to wait for it, is what the kernels' time went into (3 x 90,000 tokens x 8 heads 116 -> XX us).
+struct PageWalk {
+    const int32_t* pages;
+    int tile0, end, box_shift, page_shift, lane, batch = -1, now = 0, next = 0;
+    __device__ PageWalk(const Tables& t, const Unit& u, int tile0_, int end_) : pages(t.pages + u.page0), tile0(tile0_), end(end_), lane(threadIdx.x & 31) {
+        box_shift = 31 - __clz(min(t.page, TILE));
+        page_shift = 31 - __clz(t.page);
+        next = ask(0);
+    }
+    __device__ int ask(int i) const {            // batch i
+        const int j = tile0 + ((32 * i + lane) << box_shift);
+        return j < end ? pages[j >> page_shift] : 0;
+    }
+    __device__ int of(int box) {                 // boxes in order; the whole warp
+        if (box >> 5 != batch) {
+            batch = box >> 5;
+            now = next;
+            next = ask(batch + 1);
+        }
+        return __shfl_sync(~0u, now, box & 31);
+    }
+};
+
 // What brings a row of bf16 queries to fp16: 2^x with x = 14 less the largest exponent (top: bits of the largest magnitude); zeros,
 // infinities and NaN as they are.  Applied in two steps, as 2^x may be beyond fp32's powers.
 struct Fp16Scale {

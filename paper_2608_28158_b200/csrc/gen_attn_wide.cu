@@ -6,9 +6,8 @@
 //     O += P V             tcgen05.mma with P as the tensor-memory operand
 // Pages come by TMA, a box of up to 64 tokens of one page each.  All rows see all tokens of the run; places of a tile ahead of it or behind it
 // are taken out of S, and their values (which may be anything) are zeroed, since 0 times an infinity is not 0.
-// 8 bits: pages land in a stage of their own, and four more warps make tiles of them -- keys fp16, by one instruction a pair (the
-// queries are brought to fp16 as in the narrow kernel), values bf16 by moving bits and a multiplication by 2^120, so that p times its
-// token's power of two needs no reference of its own.  Keys' powers multiply the scores.
+// 8 bits: pages land in stages of their own, and four more warps make bf16 tiles of them, exactly: sign, exponent and fraction moved to their
+// places, times 2^120 and the token's power of two in one multiplication.
 #include "gen_attn.cuh"
 #include "kernels.h"
 
@@ -22,33 +21,50 @@ constexpr int NS = 128;                  // softmax threads, thread = row = tens
 template <bool F8>
 struct Shape {
     static constexpr int NT = NS + 64 + (F8 ? 128 : 0);            // a warp that issues the MMAs, one that asks for pages, four that widen
-    static constexpr int CTAS = F8 ? 1 : 2;
+    static constexpr int CTAS = 2;
     static constexpr int Q_BYTES = WIDE_ROWS * D * 2, KV_BYTES = TILE * D * 2, RAW = F8 ? 2 * TILE * D : 0, RAW_EXP = F8 ? 2 * TILE : 0;
-    static constexpr int RAWS = F8 ? 3 : 0;                        // stages of pages
-    static constexpr int q = 0, k = Q_BYTES, v = k + 2 * KV_BYTES, raw = v + 2 * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
-    static constexpr int bytes = misc + 2560 + 1024;
+    static constexpr int KS = F8 ? 1 : 2, RAWS = F8 ? 2 : 1;       // tiles of keys and of values; stages of 8-bit pages
+    static constexpr int q = 0, k = Q_BYTES, v = k + KS * KV_BYTES, raw = v + KS * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
+    static constexpr int bytes = misc + 256 + 1024;
 };
 constexpr int COL_S = 0, COL_O = 128, TMEM_COLS = 256;     // S / P of tile n at COL_S + 64 (n & 1)
 struct Misc {
-    float kp[2][TILE], vp[2][TILE];      // 8 bits: powers of a tile's tokens
-    float f[WIDE_ROWS];                  // what makes a row's score log2 units
-    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, raw[3], rawfree[3];
+    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, raw[2], rawfree[2];
     int dead;
     uint32_t tmem;
 };
-static_assert(sizeof(Misc) <= 2560, "misc area");
+static_assert(sizeof(Misc) <= 256, "misc area");
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// Two 8-bit values in the upper bytes of the halves of y, as bf16: sign | exponent and fraction four places down, times 2^120.
-__device__ __forceinline__ uint32_t widen_bf16(uint32_t y) {
-    const uint32_t x = ((y >> 4) & 0x07f007f0u) | (y & 0x80008000u);
+// 16 8-bit values of a token as bf16, times 2^120 and the token's power: f, and f2 where one factor cannot hold both (f2 = 1 elsewhere)
+__device__ __forceinline__ uint32_t moved(uint32_t y) { return ((y >> 4) & 0x07f007f0u) | (y & 0x80008000u); }      // from the upper bytes of the halves
+__device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f) {
     uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(0x7b807b80u));
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(f));
     return r;
+}
+__device__ __forceinline__ void widen16(const uint4& y, int exp, uint4* z) {
+    // 2^(120 + exp - 127) where that is a normal number, else 2^120 first; 255: NaN
+    const bool one = exp <= 134;
+    const uint32_t f = one ? (uint32_t)(exp + 120) << 7 : 0x7b80u, f2 = f | f << 16;
+    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        r[2 * i] = times(moved(__byte_perm(w[i], 0, 0x1404)), f2);
+        r[2 * i + 1] = times(moved(__byte_perm(w[i], 0, 0x3424)), f2);
+    }
+    if (!one) {
+        const uint32_t e = exp == 255 ? 0x7fffu : (uint32_t)exp << 7, e2 = e | e << 16;
+#pragma unroll
+        for (int i = 0; i < 8; i++) r[i] = times(r[i], e2);
+    }
+    z[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    z[1] = make_uint4(r[4], r[5], r[6], r[7]);
 }
 
 template <bool F8>
@@ -75,7 +91,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             mbar_init(&m.s[i], 1);
             mbar_init(&m.p[i], NS / 32);
         }
-        for (int i = 0; i < 3; i++) {
+        for (int i = 0; i < S::RAWS; i++) {
             mbar_init(&m.raw[i], 1);
             mbar_init(&m.rawfree[i], 4);
         }
@@ -94,19 +110,6 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             const int G = t.Hq / t.Hkv, flat = u.flat0 + i;
             x = *reinterpret_cast<const uint4*>(q + (int64_t)t.entries[u.entry + flat / G].row * ld_q + (int64_t)(h * G + flat % G) * D + ch * 8);
         }
-        if constexpr (F8) {
-            uint32_t w[4] = {x.x, x.y, x.z, x.w}, top = 0;
-#pragma unroll
-            for (int e = 0; e < 4; e++) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
-            top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
-            const Fp16Scale f(top);
-#pragma unroll
-            for (int e = 0; e < 4; e++) w[e] = f.apply(w[e]);
-            x = make_uint4(w[0], w[1], w[2], w[3]);
-            if (ch == 0) m.f[i] = f.undone(scale_log2);
-        }
         *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
     }
     fence_async_smem();
@@ -117,59 +120,65 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
 
     if (warp == NS / 32 + 1) {
         // ---- pages ---------------------------------------------------------------------------------------------------------------------
-        if (lane == 0) {
-            const int box = min(t.page, TILE), box_shift = 31 - __clz(box), page_shift = 31 - __clz(t.page);
-            for (int n = 0; n < n_tiles; n++) {
-                const int st = n & 1, rs = n % 3;
-                const int j0 = tile0 + n * TILE, boxes = (min(u.k1 - j0, TILE) + box - 1) >> box_shift;
-                auto block_of = [&](int j) { return (int64_t)t.pages[u.page0 + (j >> page_shift)] * t.Hkv + h; };
-                if constexpr (F8) {
-                    unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
-                    if (!mbar_wait(&m.rawfree[rs], ((n / 3) & 1) ^ 1, status, &m.dead)) break;
+        PageWalk walk(t, u, tile0, u.k1);
+        const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
+        for (int n = 0; n < n_tiles; n++) {
+            const int st = n % S::KS, rs = n % S::RAWS;
+            const int j0 = tile0 + n * TILE, boxes = (min(u.k1 - j0, TILE) + box - 1) >> walk.box_shift;
+            int block[4];
+#pragma unroll
+            for (int b = 0; b < 4; b++) block[b] = b < boxes ? walk.of(n * per_tile + b) * t.Hkv + h : 0;
+            auto at = [&](int b) { return (j0 + (b << walk.box_shift)) & (t.page - 1); };
+            if constexpr (F8) {
+                unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
+                if (!mbar_wait_warp(&m.rawfree[rs], ((n / S::RAWS) & 1) ^ 1, status, &m.dead)) break;
+                if (lane == 0) {
                     mbar_expect_tx(&m.raw[rs], boxes * box * (2 * D + 2));
-                    for (int b = 0; b < boxes; b++) {
-                        const int j = j0 + (b << box_shift), at = j & (t.page - 1);
-                        const int64_t block = block_of(j);
-                        tma_load_3d(raw + b * box * D, &map_k, 0, at, (int)block, &m.raw[rs]);
-                        tma_load_3d(raw + TILE * D + b * box * D, &map_v, 0, at, (int)block, &m.raw[rs]);
-                        bulk_load(exps + b * box, k_exp + block * t.page + at, box, &m.raw[rs]);
-                        bulk_load(exps + TILE + b * box, v_exp + block * t.page + at, box, &m.raw[rs]);
-                    }
-                } else {
-                    unsigned char *sk = smem + S::k + st * S::KV_BYTES, *sv = smem + S::v + st * S::KV_BYTES;
-                    if (!mbar_wait(&m.kfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
-                    mbar_expect_tx(&m.k[st], boxes * box * 2 * D);
-                    for (int b = 0; b < boxes; b++) {
-                        const int j = j0 + (b << box_shift);
-                        for (int p = 0; p < 2; p++)
-                            tma_load_3d(sk + p * (S::KV_BYTES / 2) + b * box * 128, &map_k, p * 64, j & (t.page - 1), (int)block_of(j), &m.k[st]);
-                    }
-                    if (!mbar_wait(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
-                    mbar_expect_tx(&m.v[st], boxes * box * 2 * D);
-                    for (int b = 0; b < boxes; b++) {
-                        const int j = j0 + (b << box_shift);
-                        for (int p = 0; p < 2; p++)
-                            tma_load_3d(sv + p * (S::KV_BYTES / 2) + b * box * 128, &map_v, p * 64, j & (t.page - 1), (int)block_of(j), &m.v[st]);
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        if (b >= boxes) break;
+                        tma_load_3d(raw + b * box * D, &map_k, 0, at(b), block[b], &m.raw[rs]);
+                        tma_load_3d(raw + TILE * D + b * box * D, &map_v, 0, at(b), block[b], &m.raw[rs]);
+                        bulk_load(exps + b * box, k_exp + (int64_t)block[b] * t.page + at(b), box, &m.raw[rs]);
+                        bulk_load(exps + TILE + b * box, v_exp + (int64_t)block[b] * t.page + at(b), box, &m.raw[rs]);
                     }
                 }
+            } else {
+                bool alive = true;
+#pragma unroll
+                for (int is_v = 0; is_v < 2; is_v++) {
+                    unsigned char* tile = smem + (is_v ? S::v : S::k) + st * S::KV_BYTES;
+                    uint64_t* bar = is_v ? &m.v[st] : &m.k[st];
+                    if (!(alive = mbar_wait_warp(is_v ? &m.vfree[st] : &m.kfree[st], ((n / S::KS) & 1) ^ 1, status, &m.dead))) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(bar, boxes * box * 2 * D);
+#pragma unroll
+                        for (int b = 0; b < 4; b++) {
+                            if (b >= boxes) break;
+                            for (int p = 0; p < 2; p++)
+                                tma_load_3d(tile + p * (S::KV_BYTES / 2) + b * box * 128, is_v ? &map_v : &map_k, p * 64, at(b), block[b], bar);
+                        }
+                    }
+                }
+                if (!alive) break;
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else if (warp == NS / 32) {
         // ---- MMA issue: S as wide as the tile has tokens (steps of 16), P V as deep -----------------------------------------------------------
         constexpr uint32_t I_O = instr_desc(WIDE_ROWS, D, 0, 1);
         const uint64_t dQ = desc_kmajor_base(smem_u32(smem + S::q));
         auto valid = [&](int n) { return min(u.k1 - tile0 - n * TILE, TILE); };
         auto issue_s = [&](int n) {
-            const int st = n & 1;
-            if (!mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) return false;
+            const int st = n % S::KS, b = n & 1;
+            if (!mbar_wait_warp(&m.k[st], (n / S::KS) & 1, status, &m.dead)) return false;
             tc_fence_after();
-            const uint32_t idesc = F8 ? instr_desc_f16(WIDE_ROWS, (valid(n) + 15) & ~15) : instr_desc(WIDE_ROWS, (valid(n) + 15) & ~15, 0, 0);
+            const uint32_t idesc = instr_desc(WIDE_ROWS, (valid(n) + 15) & ~15, 0, 0);
             const uint64_t dK = desc_kmajor_base(smem_u32(smem + S::k + st * S::KV_BYTES));
             if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ks++) mma_ss(tmem + COL_S + st * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks), dK + kstep_kmajor<TILE>(ks), idesc, ks > 0);
-                mma_commit(&m.s[st]);
+                for (int ks = 0; ks < 8; ks++) mma_ss(tmem + COL_S + b * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks), dK + kstep_kmajor<TILE>(ks), idesc, ks > 0);
+                mma_commit(&m.s[b]);
                 mma_commit(&m.kfree[st]);
             }
             __syncwarp();
@@ -177,11 +186,11 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         };
         bool alive = issue_s(0);
         for (int n = 0; n < n_tiles && alive; n++) {
-            const int st = n & 1, steps = (valid(n) + 15) >> 4;
+            const int st = n % S::KS, b = n & 1, steps = (valid(n) + 15) >> 4;
             // S of tile n + 1 goes to the other buffer and runs under the softmax of tile n (that buffer's P was read by the P V
             // MMAs of tile n - 1, which precede it in the pipe)
             if (n + 1 < n_tiles && !(alive = issue_s(n + 1))) break;
-            if (!(alive = mbar_wait_warp(&m.v[st], (n >> 1) & 1, status, &m.dead))) break;
+            if (!(alive = mbar_wait_warp(&m.v[st], (n / S::KS) & 1, status, &m.dead))) break;
             if (!F8 && (valid(n) < steps * 16 || (n == 0 && tile0 < u.k0))) {      // (8 bits: zeroed where they are widened)
                 unsigned char* sv = smem + S::v + st * S::KV_BYTES;
                 for (int e = lane; e < TILE * 16; e += 32) {
@@ -192,13 +201,13 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
                 fence_async_smem();
                 __syncwarp();
             }
-            if (!(alive = mbar_wait_warp(&m.p[st], (n >> 1) & 1, status, &m.dead))) break;
+            if (!(alive = mbar_wait_warp(&m.p[b], (n >> 1) & 1, status, &m.dead))) break;
             tc_fence_after();
             const uint64_t dV = desc_mnmajor_base<TILE>(smem_u32(smem + S::v + st * S::KV_BYTES));
             if (elect_one()) {
 #pragma unroll 1
                 for (int ks = 0; ks < steps; ks++)
-                    mma_ts(tmem + COL_O, tmem + COL_S + st * 64 + ks * 8, dV + kstep_mnmajor(ks), I_O, n > 0 || ks > 0);
+                    mma_ts(tmem + COL_O, tmem + COL_S + b * 64 + ks * 8, dV + kstep_mnmajor(ks), I_O, n > 0 || ks > 0);
                 mma_commit(&m.pv);                                    // one phase per tile, in order
                 mma_commit(&m.vfree[st]);
                 if (n + 1 == n_tiles) mma_commit(&m.o);
@@ -207,95 +216,63 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         }
     } else if (F8 && warp >= NS / 32 + 2) {
         // ---- 8-bit pages -> tiles ---------------------------------------------------------------------------------------------------------
-        const int wt = tid - NS - 64;
+        // a quarter of a warp stores to eight different places of two keys' rows of 128 bytes
+        const int wt = tid - NS - 64, ch0 = wt & 3, key0 = wt >> 2;
         for (int n = 0; n < n_tiles; n++) {
-            const int st = n & 1, rs = n % 3, j0 = tile0 + n * TILE;
-            if (!mbar_wait_warp(&m.raw[rs], (n / 3) & 1, status, &m.dead)) break;
-            // the powers' places are free when P of two tiles ago has been used
-            if (!mbar_wait_warp(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
-            if (!mbar_wait_warp(&m.kfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+            const int st = n % S::KS, rs = n % S::RAWS, j0 = tile0 + n * TILE;
+            if (!mbar_wait_warp(&m.raw[rs], (n / S::RAWS) & 1, status, &m.dead)) break;
             const unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
-            unsigned char *sk = smem + S::k + st * S::KV_BYTES, *sv = smem + S::v + st * S::KV_BYTES;
-            if (wt < TILE) m.kp[st][wt] = gen_power(exps[wt]);
-            else m.vp[st][wt - TILE] = gen_power(exps[wt]);
+#pragma unroll 1
+            for (int is_v = 0; is_v < 2; is_v++) {
+                if (!mbar_wait_warp(is_v ? &m.vfree[st] : &m.kfree[st], ((n / S::KS) & 1) ^ 1, status, &m.dead)) break;
+                unsigned char* tile = smem + (is_v ? S::v : S::k) + st * S::KV_BYTES;
 #pragma unroll
-            for (int x = 0; x < 4; x++) {                             // 16 features of a key each
-                const int e = wt + 128 * x, key = e >> 3, ch = e & 7;
-                const uint4 y = *reinterpret_cast<const uint4*>(raw + sw128_chunk(key, ch));
-                unsigned char* dst = sk + (ch >> 2) * (S::KV_BYTES / 2);
-                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch) & 7)) = make_uint4(widen(y.x), widen_upper(y.x), widen(y.y), widen_upper(y.y));
-                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch + 1) & 7)) = make_uint4(widen(y.z), widen_upper(y.z), widen(y.w), widen_upper(y.w));
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&m.k[st]);
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-                const int e = wt + 128 * x, key = e >> 3, ch = e & 7;
-                uint4 y = *reinterpret_cast<const uint4*>(raw + TILE * D + sw128_chunk(key, ch));
-                if (j0 + key < u.k0 || j0 + key >= u.k1) y = make_uint4(0, 0, 0, 0);
-                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-                uint32_t z[8];
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    z[2 * i] = widen_bf16(__byte_perm(w[i], 0, 0x1404));
-                    z[2 * i + 1] = widen_bf16(__byte_perm(w[i], 0, 0x3424));
-                    if (__vcmpeq4(w[i] & 0x7f7f7f7fu, 0x7f7f7f7fu)) {          // a NaN byte
-                        auto nan_or = [&](uint32_t v, int b) {
-                            return v | ((w[i] >> b & 0x7fu) == 0x7fu ? 0x7fffu : 0u) | ((w[i] >> (b + 8) & 0x7fu) == 0x7fu ? 0x7fff0000u : 0u);
-                        };
-                        z[2 * i] = nan_or(z[2 * i], 0);
-                        z[2 * i + 1] = nan_or(z[2 * i + 1], 16);
-                    }
+                for (int x = 0; x < 4; x++) {                         // 16 features of a token each
+                    const int key = key0 + 32 * (x >> 1), ch = ch0 + 4 * (x & 1);
+                    uint4 y = *reinterpret_cast<const uint4*>(raw + is_v * TILE * D + sw128_chunk(key, ch)), z[2];
+                    int exp = exps[is_v * TILE + key];
+                    // values of other tokens may be anything: zeros
+                    if (is_v && (j0 + key < u.k0 || j0 + key >= u.k1)) y = make_uint4(0, 0, 0, 0), exp = 127;
+                    widen16(y, exp, z);
+                    unsigned char* dst = tile + (ch >> 2) * (S::KV_BYTES / 2);
+                    *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0)) = z[0];
+                    *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0 + 1)) = z[1];
                 }
-                unsigned char* dst = sv + (ch >> 2) * (S::KV_BYTES / 2);
-                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch) & 7)) = make_uint4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, (2 * ch + 1) & 7)) = make_uint4(z[4], z[5], z[6], z[7]);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(is_v ? &m.v[st] : &m.k[st]);
             }
-            fence_async_smem();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(&m.v[st]);
-                mbar_arrive(&m.rawfree[rs]);
-            }
+            if (lane == 0) mbar_arrive(&m.rawfree[rs]);
         }
     } else {
         // ---- softmax: a row per thread -----------------------------------------------------------------------------------------------------
         const uint32_t tm_lane = tmem + ((uint32_t)(warp * 32) << 16);
-        const float f = F8 ? m.f[tid] : scale_log2;
-        const F2 f2v = f2(f, f);
+        const F2 scale2 = f2(scale_log2, scale_log2);
         float m_ref = -INFINITY, l_sum = 0.f;
         for (int n = 0; n < n_tiles; n++) {
-            const int st = n & 1, j0 = tile0 + n * TILE;
-            if (!mbar_wait_warp(&m.s[st], (n >> 1) & 1, status, &m.dead)) break;
-            if (F8 && !mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) break;        // (complete: orders the powers)
+            const int b = n & 1, j0 = tile0 + n * TILE;
+            if (!mbar_wait_warp(&m.s[b], (n >> 1) & 1, status, &m.dead)) break;
             tc_fence_after();
-            uint32_t x[TILE];
-            tmem_ld32(tm_lane + COL_S + st * 64, x);
-            tmem_ld32(tm_lane + COL_S + st * 64 + 32, x + 32);
-            tmem_ld_wait();
-            if constexpr (F8) {
+            const bool edge = j0 < u.k0 || j0 + TILE > u.k1;
+            float mx = -INFINITY;
+            uint32_t x[32];                           // half a row of S at a time, so that two CTAs' registers fit
+            auto half = [&](int c) {
+                tmem_ld32(tm_lane + COL_S + b * 64 + c * 32, x);
+                tmem_ld_wait();
+                if (edge) {
 #pragma unroll
-                for (int e = 0; e < TILE; e += 4) {
-                    const float4 kp = *reinterpret_cast<const float4*>(&m.kp[st][e]);
-                    float a, b;
-                    f2_split(f2_mul(f2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), f2(kp.x, kp.y)), a, b);
-                    x[e] = __float_as_uint(a);
-                    x[e + 1] = __float_as_uint(b);
-                    f2_split(f2_mul(f2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), f2(kp.z, kp.w)), a, b);
-                    x[e + 2] = __float_as_uint(a);
-                    x[e + 3] = __float_as_uint(b);
+                    for (int e = 0; e < 32; e++)
+                        if (j0 + c * 32 + e < u.k0 || j0 + c * 32 + e >= u.k1) x[e] = __float_as_uint(-INFINITY);
                 }
-            }
-            if (j0 < u.k0 || j0 + TILE > u.k1) {
+            };
 #pragma unroll
-                for (int e = 0; e < TILE; e++)
-                    if (j0 + e < u.k0 || j0 + e >= u.k1) x[e] = __float_as_uint(-INFINITY);
-            }
-            float mx = __uint_as_float(x[0]);
+            for (int c = 1; c >= 0; c--) {
+                half(c);
 #pragma unroll
-            for (int e = 1; e + 1 < TILE; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-            mx = fmaxf(mx, __uint_as_float(x[TILE - 1])) * f;
+                for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+            }
+            mx *= scale_log2;
             const bool raise = mx > m_ref + RAISE || (m_ref == -INFINITY && mx > -INFINITY);
             if (__any_sync(~0u, raise && n > 0)) {
                 // O is about to be read and rewritten: the P V MMAs of the tile before must be done (this warp is never more than a phase behind)
@@ -322,22 +299,18 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             F2 part[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
             for (int c = 0; c < 2; c++) {
+                if (c == 1) half(1);                      // (the first half is still there)
                 uint32_t pk[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
                     float p0, p1;
-                    f2_split(f2_fma(f2(__uint_as_float(x[c * 32 + e]), __uint_as_float(x[c * 32 + e + 1])), f2v, nm), p0, p1);
+                    f2_split(f2_fma(f2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), scale2, nm), p0, p1);
                     p0 = ex2(p0);
                     p1 = ex2(p1);
                     part[(e >> 1) & 1] = f2_add(part[(e >> 1) & 1], f2(p0, p1));
-                    if constexpr (F8) {
-                        const float2 vp = *reinterpret_cast<const float2*>(&m.vp[st][c * 32 + e]);
-                        p0 = p0 == 0.f ? 0.f : p0 * vp.x;             // (behind the run a power may be anything)
-                        p1 = p1 == 0.f ? 0.f : p1 * vp.y;
-                    }
                     pk[e >> 1] = pack_bf16(p0, p1);
                 }
-                tmem_st16(tm_lane + COL_S + st * 64 + c * 16, pk);
+                tmem_st16(tm_lane + COL_S + b * 64 + c * 16, pk);      // (over what of S has been read: its first half)
             }
             float a0, a1;
             f2_split(f2_add(part[0], part[1]), a0, a1);
@@ -345,7 +318,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&m.p[st]);
+            if (lane == 0) mbar_arrive(&m.p[b]);
         }
         // ---- O / l, and its place -----------------------------------------------------------------------------------------------------------
         const bool ok = mbar_wait_warp(&m.o, 0, status, &m.dead);
