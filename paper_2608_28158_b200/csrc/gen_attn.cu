@@ -153,11 +153,14 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 top = max(top & 0xffffu, top >> 16);
                 top = max(top, __shfl_xor_sync(~0u, top, 1));
                 top = max(top, __shfl_xor_sync(~0u, top, 2));
-                const Fp16Scale x(top);
+                const PowerOfTwo x(top, 14);         // fp16; what falls below 2^-24 is 2^-38 of the largest
 #pragma unroll
                 for (int ks = 0; ks < 8; ks++)
 #pragma unroll
-                    for (int y = 0; y < 2; y++) qb[r][ks][y] = x.apply(qb[r][ks][y]);
+                    for (int y = 0; y < 2; y++) {
+                        const float2 z = x.apply(qb[r][ks][y]);
+                        qb[r][ks][y] = pack_f16(z.x, z.y);
+                    }
                 own = x.undone(scale_log2);
             }
 #pragma unroll

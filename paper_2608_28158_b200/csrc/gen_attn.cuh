@@ -84,20 +84,20 @@ struct PageWalk {
     }
 };
 
-// What brings a row of bf16 queries to fp16: 2^x with x = 14 less the largest exponent (top: bits of the largest magnitude); zeros,
+// What brings a row of bf16 queries to 2^to: 2^x with x = to less the largest exponent (top: bits of the largest magnitude); zeros,
 // infinities and NaN as they are.  Applied in two steps, as 2^x may be beyond fp32's powers.
-struct Fp16Scale {
+struct PowerOfTwo {
     float f1, f2;
     int x1, x2;
-    __device__ __forceinline__ explicit Fp16Scale(uint32_t top) {
-        const int e = (int)(top >> 7), x = e == 0 || e == 255 ? 0 : 141 - e;
+    __device__ __forceinline__ PowerOfTwo(uint32_t top, int to) {
+        const int e = (int)(top >> 7), x = e == 0 || e == 255 ? 0 : to + 127 - e;
         x1 = x / 2;
         x2 = x - x1;
         f1 = __uint_as_float((uint32_t)(127 + x1) << 23);
         f2 = __uint_as_float((uint32_t)(127 + x2) << 23);
     }
-    __device__ __forceinline__ uint32_t apply(uint32_t pair) const {
-        return pack_f16(__uint_as_float(pair << 16) * f1 * f2, __uint_as_float(pair & 0xffff0000u) * f1 * f2);
+    __device__ __forceinline__ float2 apply(uint32_t pair) const {
+        return make_float2(__uint_as_float(pair << 16) * f1 * f2, __uint_as_float(pair & 0xffff0000u) * f1 * f2);
     }
     __device__ __forceinline__ float undone(float scale) const {
         return scale * __uint_as_float((uint32_t)(127 - x1) << 23) * __uint_as_float((uint32_t)(127 - x2) << 23);

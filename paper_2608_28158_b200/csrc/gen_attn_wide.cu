@@ -6,8 +6,14 @@
 //     O += P V             tcgen05.mma with P as the tensor-memory operand
 // Pages come by TMA, a box of up to 64 tokens of one page each.  All rows see all tokens of the run; places of a tile ahead of it or behind it
 // are taken out of S, and their values (which may be anything) are zeroed, since 0 times an infinity is not 0.
-// 8 bits: pages land in stages of their own, and four more warps make bf16 tiles of them, exactly: sign, exponent and fraction moved to their
-// places, times 2^120 and the token's power of two in one multiplication.
+// 8 bits: keys go into the first product as they are.  A query is two 8-bit terms for it (a row brought to 2^7 by a power of two; its 8
+// significant bits are 4 and 4, and what the second term loses below 2^-9 is 2^-18 of the row's largest), so S is two products of twice the rate.
+// Values become bf16 tiles, exactly, by four more warps: sign, exponent and fraction moved to their places, times 2^120 and the
+// token's power of two in one multiplication.  A key's power multiplies its scores.
+#include <cuda_fp8.h>
+
+#include <cstddef>
+
 #include "gen_attn.cuh"
 #include "kernels.h"
 
@@ -23,17 +29,18 @@ struct Shape {
     static constexpr int NT = NS + 64 + (F8 ? 128 : 0);            // a warp that issues the MMAs, one that asks for pages, four that widen
     static constexpr int CTAS = 2;
     static constexpr int Q_BYTES = WIDE_ROWS * D * 2, KV_BYTES = TILE * D * 2, RAW = F8 ? 2 * TILE * D : 0, RAW_EXP = F8 ? 2 * TILE : 0;
-    static constexpr int KS = F8 ? 1 : 2, RAWS = F8 ? 2 : 1;       // tiles of keys and of values; stages of 8-bit pages
-    static constexpr int q = 0, k = Q_BYTES, v = k + KS * KV_BYTES, raw = v + KS * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
-    static constexpr int bytes = misc + 256 + 1024;
+    static constexpr int RAWS = 2, KB = F8 ? 0 : 2 * KV_BYTES;     // stages of 8-bit pages; tiles of bf16 keys
+    static constexpr int q = 0, k = Q_BYTES, v = k + KB, raw = v + 2 * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
+    static constexpr int bytes = misc + (F8 ? 1280 : 256) + 1024;
 };
 constexpr int COL_S = 0, COL_O = 128, TMEM_COLS = 256;     // S / P of tile n at COL_S + 64 (n & 1)
 struct Misc {
-    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, raw[2], rawfree[2];
+    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, kp_full[2];      // 8 bits: k, kfree are those of the stages of pages
     int dead;
     uint32_t tmem;
+    float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: powers of a tile's keys, and what makes a row's score log2 units
 };
-static_assert(sizeof(Misc) <= 256, "misc area");
+static_assert(offsetof(Misc, kp) <= 256 && sizeof(Misc) <= 1280, "misc area");
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
@@ -67,6 +74,13 @@ __device__ __forceinline__ void widen16(const uint4& y, int exp, uint4* z) {
     z[1] = make_uint4(r[4], r[5], r[6], r[7]);
 }
 
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+                 "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+// e4m3 inputs, fp32 sums, both K-major
+__host__ __device__ constexpr uint32_t instr_desc_f8(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+
 template <bool F8>
 __global__ void __launch_bounds__(Shape<F8>::NT, Shape<F8>::CTAS)
 wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, const __grid_constant__ CUtensorMap map_k,
@@ -81,19 +95,16 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
     let_next_launch();
     const Unit u = t.units[blockIdx.x / t.Hkv];
     const int h = blockIdx.x % t.Hkv;
-    const int tile0 = u.k0 & ~(TILE - 1), n_tiles = (u.k1 - tile0 + TILE - 1) / TILE;
+    const int tile0 = u.k0 & ~(TILE - 1), n_tiles = (u.k1 - tile0 + TILE - 1) / TILE, active = (u.n + 31) / 32;      // (warps that have rows)
     if (tid == 0) {
         for (int i = 0; i < 2; i++) {
-            mbar_init(&m.k[i], F8 ? 4 : 1);
+            mbar_init(&m.k[i], 1);
             mbar_init(&m.v[i], F8 ? 4 : 1);
-            mbar_init(&m.kfree[i], 1);
+            mbar_init(&m.kfree[i], F8 ? 5 : 1);             // the product that read it, and the warps that widen
             mbar_init(&m.vfree[i], 1);
             mbar_init(&m.s[i], 1);
-            mbar_init(&m.p[i], NS / 32);
-        }
-        for (int i = 0; i < S::RAWS; i++) {
-            mbar_init(&m.raw[i], 1);
-            mbar_init(&m.rawfree[i], 4);
+            mbar_init(&m.p[i], active);
+            mbar_init(&m.kp_full[i], 2);
         }
         mbar_init(&m.pv, 1);
         mbar_init(&m.o, 1);
@@ -110,7 +121,31 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             const int G = t.Hq / t.Hkv, flat = u.flat0 + i;
             x = *reinterpret_cast<const uint4*>(q + (int64_t)t.entries[u.entry + flat / G].row * ld_q + (int64_t)(h * G + flat % G) * D + ch * 8);
         }
-        *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
+        if constexpr (F8) {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            uint32_t top = 0, hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; e++) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
+            top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+            const PowerOfTwo f(top, 7);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const float2 y = f.apply(w[e]);
+                const uint32_t y8 = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
+                const uint32_t y16 = widen(y8);
+                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&y16));
+                hi[e >> 1] |= y8 << (16 * (e & 1));
+                lo[e >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y.x - back.x, y.y - back.y), __NV_SATFINITE, __NV_E4M3) << (16 * (e & 1));
+            }
+            unsigned char* dst = smem + S::q + sw128_chunk(i, ch >> 1) + 8 * (ch & 1);
+            *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
+            *reinterpret_cast<uint2*>(dst + S::Q_BYTES / 2) = make_uint2(lo[0], lo[1]);
+            if (ch == 0) m.f[i] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : f.undone(scale_log2);      // infinite or NaN: NaN
+        } else {
+            *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
+        }
     }
     fence_async_smem();
     tc_fence_before();
@@ -123,24 +158,24 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         PageWalk walk(t, u, tile0, u.k1);
         const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
         for (int n = 0; n < n_tiles; n++) {
-            const int st = n % S::KS, rs = n % S::RAWS;
+            const int st = n & 1, ph = ((n >> 1) & 1) ^ 1;
             const int j0 = tile0 + n * TILE, boxes = (min(u.k1 - j0, TILE) + box - 1) >> walk.box_shift;
             int block[4];
 #pragma unroll
             for (int b = 0; b < 4; b++) block[b] = b < boxes ? walk.of(n * per_tile + b) * t.Hkv + h : 0;
             auto at = [&](int b) { return (j0 + (b << walk.box_shift)) & (t.page - 1); };
             if constexpr (F8) {
-                unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
-                if (!mbar_wait_warp(&m.rawfree[rs], ((n / S::RAWS) & 1) ^ 1, status, &m.dead)) break;
+                unsigned char *raw = smem + S::raw + st * S::RAW, *exps = smem + S::raw_exp + st * S::RAW_EXP;
+                if (!mbar_wait_warp(&m.kfree[st], ph, status, &m.dead)) break;
                 if (lane == 0) {
-                    mbar_expect_tx(&m.raw[rs], boxes * box * (2 * D + 2));
+                    mbar_expect_tx(&m.k[st], boxes * box * (2 * D + 2));
 #pragma unroll
                     for (int b = 0; b < 4; b++) {
                         if (b >= boxes) break;
-                        tma_load_3d(raw + b * box * D, &map_k, 0, at(b), block[b], &m.raw[rs]);
-                        tma_load_3d(raw + TILE * D + b * box * D, &map_v, 0, at(b), block[b], &m.raw[rs]);
-                        bulk_load(exps + b * box, k_exp + (int64_t)block[b] * t.page + at(b), box, &m.raw[rs]);
-                        bulk_load(exps + TILE + b * box, v_exp + (int64_t)block[b] * t.page + at(b), box, &m.raw[rs]);
+                        tma_load_3d(raw + b * box * D, &map_k, 0, at(b), block[b], &m.k[st]);
+                        tma_load_3d(raw + TILE * D + b * box * D, &map_v, 0, at(b), block[b], &m.k[st]);
+                        bulk_load(exps + b * box, k_exp + (int64_t)block[b] * t.page + at(b), box, &m.k[st]);
+                        bulk_load(exps + TILE + b * box, v_exp + (int64_t)block[b] * t.page + at(b), box, &m.k[st]);
                     }
                 }
             } else {
@@ -149,7 +184,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
                 for (int is_v = 0; is_v < 2; is_v++) {
                     unsigned char* tile = smem + (is_v ? S::v : S::k) + st * S::KV_BYTES;
                     uint64_t* bar = is_v ? &m.v[st] : &m.k[st];
-                    if (!(alive = mbar_wait_warp(is_v ? &m.vfree[st] : &m.kfree[st], ((n / S::KS) & 1) ^ 1, status, &m.dead))) break;
+                    if (!(alive = mbar_wait_warp(is_v ? &m.vfree[st] : &m.kfree[st], ph, status, &m.dead))) break;
                     if (lane == 0) {
                         mbar_expect_tx(bar, boxes * box * 2 * D);
 #pragma unroll
@@ -170,15 +205,20 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         const uint64_t dQ = desc_kmajor_base(smem_u32(smem + S::q));
         auto valid = [&](int n) { return min(u.k1 - tile0 - n * TILE, TILE); };
         auto issue_s = [&](int n) {
-            const int st = n % S::KS, b = n & 1;
-            if (!mbar_wait_warp(&m.k[st], (n / S::KS) & 1, status, &m.dead)) return false;
+            const int st = n & 1, width = (valid(n) + 15) & ~15;
+            if (!mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) return false;
             tc_fence_after();
-            const uint32_t idesc = instr_desc(WIDE_ROWS, (valid(n) + 15) & ~15, 0, 0);
-            const uint64_t dK = desc_kmajor_base(smem_u32(smem + S::k + st * S::KV_BYTES));
+            const uint64_t dK = desc_kmajor_base(smem_u32(smem + (F8 ? S::raw + st * S::RAW : S::k + st * S::KV_BYTES)));
             if (elect_one()) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ks++) mma_ss(tmem + COL_S + b * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks), dK + kstep_kmajor<TILE>(ks), idesc, ks > 0);
-                mma_commit(&m.s[b]);
+                for (int ks = 0; ks < 8; ks++) {
+                    if constexpr (F8)        // 32 features a step: the first terms of all, then the second
+                        mma_f8(tmem + COL_S + st * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks & 3) + (ks >> 2) * (S::Q_BYTES / 2 >> 4), dK + kstep_kmajor<TILE>(ks & 3),
+                               instr_desc_f8(WIDE_ROWS, width), ks > 0);
+                    else
+                        mma_ss(tmem + COL_S + st * 64, dQ + kstep_kmajor<WIDE_ROWS>(ks), dK + kstep_kmajor<TILE>(ks), instr_desc(WIDE_ROWS, width, 0, 0), ks > 0);
+                }
+                mma_commit(&m.s[st]);
                 mma_commit(&m.kfree[st]);
             }
             __syncwarp();
@@ -186,11 +226,11 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         };
         bool alive = issue_s(0);
         for (int n = 0; n < n_tiles && alive; n++) {
-            const int st = n % S::KS, b = n & 1, steps = (valid(n) + 15) >> 4;
+            const int st = n & 1, steps = (valid(n) + 15) >> 4;
             // S of tile n + 1 goes to the other buffer and runs under the softmax of tile n (that buffer's P was read by the P V
             // MMAs of tile n - 1, which precede it in the pipe)
             if (n + 1 < n_tiles && !(alive = issue_s(n + 1))) break;
-            if (!(alive = mbar_wait_warp(&m.v[st], (n / S::KS) & 1, status, &m.dead))) break;
+            if (!(alive = mbar_wait_warp(&m.v[st], (n >> 1) & 1, status, &m.dead))) break;
             if (!F8 && (valid(n) < steps * 16 || (n == 0 && tile0 < u.k0))) {      // (8 bits: zeroed where they are widened)
                 unsigned char* sv = smem + S::v + st * S::KV_BYTES;
                 for (int e = lane; e < TILE * 16; e += 32) {
@@ -201,13 +241,13 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
                 fence_async_smem();
                 __syncwarp();
             }
-            if (!(alive = mbar_wait_warp(&m.p[b], (n >> 1) & 1, status, &m.dead))) break;
+            if (!(alive = mbar_wait_warp(&m.p[st], (n >> 1) & 1, status, &m.dead))) break;
             tc_fence_after();
             const uint64_t dV = desc_mnmajor_base<TILE>(smem_u32(smem + S::v + st * S::KV_BYTES));
             if (elect_one()) {
 #pragma unroll 1
                 for (int ks = 0; ks < steps; ks++)
-                    mma_ts(tmem + COL_O, tmem + COL_S + b * 64 + ks * 8, dV + kstep_mnmajor(ks), I_O, n > 0 || ks > 0);
+                    mma_ts(tmem + COL_O, tmem + COL_S + st * 64 + ks * 8, dV + kstep_mnmajor(ks), I_O, n > 0 || ks > 0);
                 mma_commit(&m.pv);                                    // one phase per tile, in order
                 mma_commit(&m.vfree[st]);
                 if (n + 1 == n_tiles) mma_commit(&m.o);
@@ -219,40 +259,45 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         // a quarter of a warp stores to eight different places of two keys' rows of 128 bytes
         const int wt = tid - NS - 64, ch0 = wt & 3, key0 = wt >> 2;
         for (int n = 0; n < n_tiles; n++) {
-            const int st = n % S::KS, rs = n % S::RAWS, j0 = tile0 + n * TILE;
-            if (!mbar_wait_warp(&m.raw[rs], (n / S::RAWS) & 1, status, &m.dead)) break;
-            const unsigned char *raw = smem + S::raw + rs * S::RAW, *exps = smem + S::raw_exp + rs * S::RAW_EXP;
-#pragma unroll 1
-            for (int is_v = 0; is_v < 2; is_v++) {
-                if (!mbar_wait_warp(is_v ? &m.vfree[st] : &m.kfree[st], ((n / S::KS) & 1) ^ 1, status, &m.dead)) break;
-                unsigned char* tile = smem + (is_v ? S::v : S::k) + st * S::KV_BYTES;
-#pragma unroll
-                for (int x = 0; x < 4; x++) {                         // 16 features of a token each
-                    const int key = key0 + 32 * (x >> 1), ch = ch0 + 4 * (x & 1);
-                    uint4 y = *reinterpret_cast<const uint4*>(raw + is_v * TILE * D + sw128_chunk(key, ch)), z[2];
-                    int exp = exps[is_v * TILE + key];
-                    // values of other tokens may be anything: zeros
-                    if (is_v && (j0 + key < u.k0 || j0 + key >= u.k1)) y = make_uint4(0, 0, 0, 0), exp = 127;
-                    widen16(y, exp, z);
-                    unsigned char* dst = tile + (ch >> 2) * (S::KV_BYTES / 2);
-                    *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0)) = z[0];
-                    *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0 + 1)) = z[1];
-                }
-                fence_async_smem();
+            const int st = n & 1, j0 = tile0 + n * TILE;
+            if (!mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) break;
+            // (P of two tiles ago has been used: so have its keys' powers)
+            if (!mbar_wait_warp(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
+            const unsigned char *raw = smem + S::raw + st * S::RAW + TILE * D, *exps = smem + S::raw_exp + st * S::RAW_EXP;
+            if (wt < TILE) {
+                m.kp[st][wt] = gen_power(exps[wt]);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(is_v ? &m.v[st] : &m.k[st]);
+                if (lane == 0) mbar_arrive(&m.kp_full[st]);
             }
+            unsigned char* tile = smem + S::v + st * S::KV_BYTES;
+#pragma unroll 2
+            for (int x = 0; x < 4; x++) {                             // 16 features of a token each
+                const int key = key0 + 32 * (x >> 1), ch = ch0 + 4 * (x & 1);
+                uint4 y = *reinterpret_cast<const uint4*>(raw + sw128_chunk(key, ch)), z[2];
+                int exp = exps[TILE + key];
+                if (j0 + key < u.k0 || j0 + key >= u.k1) y = make_uint4(0, 0, 0, 0), exp = 127;      // others' may be anything: zeros
+                widen16(y, exp, z);
+                unsigned char* dst = tile + (ch >> 2) * (S::KV_BYTES / 2);
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0)) = z[0];
+                *reinterpret_cast<uint4*>(dst + sw128_chunk(key, 2 * ch0 + 1)) = z[1];
+            }
+            fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&m.rawfree[rs]);
+            if (lane == 0) {
+                mbar_arrive(&m.v[st]);
+                mbar_arrive(&m.kfree[st]);
+            }
         }
-    } else {
+    } else if (warp < active) {
         // ---- softmax: a row per thread -----------------------------------------------------------------------------------------------------
         const uint32_t tm_lane = tmem + ((uint32_t)(warp * 32) << 16);
-        const F2 scale2 = f2(scale_log2, scale_log2);
+        const float scale = F8 ? m.f[tid] : scale_log2;
+        const F2 scale2 = f2(scale, scale);
         float m_ref = -INFINITY, l_sum = 0.f;
         for (int n = 0; n < n_tiles; n++) {
             const int b = n & 1, j0 = tile0 + n * TILE;
             if (!mbar_wait_warp(&m.s[b], (n >> 1) & 1, status, &m.dead)) break;
+            if (F8 && !mbar_wait_warp(&m.kp_full[b], (n >> 1) & 1, status, &m.dead)) break;
             tc_fence_after();
             const bool edge = j0 < u.k0 || j0 + TILE > u.k1;
             float mx = -INFINITY;
@@ -260,6 +305,17 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             auto half = [&](int c) {
                 tmem_ld32(tm_lane + COL_S + b * 64 + c * 32, x);
                 tmem_ld_wait();
+                if constexpr (F8) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 kp = *reinterpret_cast<const float4*>(&m.kp[b][c * 32 + e]);
+                        float y[4];
+                        f2_split(f2_mul(f2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), f2(kp.x, kp.y)), y[0], y[1]);
+                        f2_split(f2_mul(f2(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])), f2(kp.z, kp.w)), y[2], y[3]);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) x[e + i] = __float_as_uint(y[i]);
+                    }
+                }
                 if (edge) {
 #pragma unroll
                     for (int e = 0; e < 32; e++)
@@ -272,7 +328,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
             }
-            mx *= scale_log2;
+            mx *= scale;
             const bool raise = mx > m_ref + RAISE || (m_ref == -INFINITY && mx > -INFINITY);
             if (__any_sync(~0u, raise && n > 0)) {
                 // O is about to be read and rewritten: the P V MMAs of the tile before must be done (this warp is never more than a phase behind)
@@ -281,14 +337,14 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
                 const float m_new = raise ? mx : m_ref;
                 const float alpha = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
                 l_sum *= alpha;
-#pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    uint32_t y[32];
-                    tmem_ld32(tm_lane + COL_O + c * 32, y);
+#pragma unroll 1
+                for (int c = 0; c < 8; c++) {
+                    uint32_t y[16];
+                    tmem_ld16(tm_lane + COL_O + c * 16, y);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
-                    tmem_st32(tm_lane + COL_O + c * 32, y);
+                    for (int e = 0; e < 16; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+                    tmem_st16(tm_lane + COL_O + c * 16, y);
                 }
                 m_ref = m_new;
             } else if (raise) {
@@ -332,24 +388,26 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             if (r.alone) lse[out] = l2 * LN2;
             else part_lse[part] = l2;
         }
-#pragma unroll
-        for (int c = 0; c < 4; c++) {
-            uint32_t x[32];
-            tmem_ld32(tm_lane + COL_O + c * 32, x);
+#pragma unroll 1
+        for (int c = 0; c < 8; c++) {
+            uint32_t x[16];
+            tmem_ld16(tm_lane + COL_O + c * 16, x);
             tmem_ld_wait();
-            if (!mine) continue;
+            if (mine) {
 #pragma unroll
-            for (int e = 0; e < 32; e++) x[e] = __float_as_uint(__uint_as_float(x[e]) * inv);
-            if (r.alone) {
+                for (int e = 0; e < 16; e++) x[e] = __float_as_uint(__uint_as_float(x[e]) * inv);
+                if (r.alone) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 8)
-                    *reinterpret_cast<uint4*>(o + out * D + c * 32 + e) =
-                        make_uint4(pack_bf16(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pack_bf16(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])),
-                                   pack_bf16(__uint_as_float(x[e + 4]), __uint_as_float(x[e + 5])), pack_bf16(__uint_as_float(x[e + 6]), __uint_as_float(x[e + 7])));
-            } else {
+                    for (int e = 0; e < 16; e += 8)
+                        *reinterpret_cast<uint4*>(o + out * D + c * 16 + e) =
+                            make_uint4(pack_bf16(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pack_bf16(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3])),
+                                       pack_bf16(__uint_as_float(x[e + 4]), __uint_as_float(x[e + 5])), pack_bf16(__uint_as_float(x[e + 6]), __uint_as_float(x[e + 7])));
+                } else {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(part_o + part * D + c * 32 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                    for (int e = 0; e < 16; e += 4) *reinterpret_cast<uint4*>(part_o + part * D + c * 16 + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                }
             }
+            __syncwarp();
         }
     }
     __syncwarp();
