@@ -2,6 +2,7 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -56,7 +57,7 @@ int32_t gen_cache_read(const GenCache& c, const GenRows& r);
 
 // Index of harts_gen_attn_index: header words, then the arrays (gen_attn_host.cc writes it, gen_attn.cu reads it).
 namespace gen_attn {
-enum Header { N_Q, HQ, HKV, PAGE, N_NARROW, N_WIDE, N_PARTS, MERGED, MAX_PAGE, WORDS, NARROW, WIDE, ENTRY, PAGES, PART_PTR, PART, NARROW_MAX };
+enum Header { N_Q, HQ, HKV, PAGE, N_NARROW, N_WIDE, N_PARTS, MERGED, MAX_PAGE, WORDS, NARROW, WIDE, ENTRY, PAGES, PART_PTR, PART, NARROW_MAX, N_LISTS, LIST_PTR };
 constexpr int NARROW_ROWS = 16, WIDE_ROWS = 128;
 struct Unit {                 // rows that read the same tokens of a node: rows flat0 .. flat0 + n - 1 of (entry, head of the group)
     int32_t entry, flat0, n, k0, k1, page0, part0, pad;
@@ -70,6 +71,18 @@ struct Entry {                // a query that sees tokens of a node
 }  // namespace gen_attn
 int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int64_t ld_q, const GenCache& c, const int32_t* q_pos, void* o,
                  float* lse, float scale, void* workspace, int32_t* dev_status, cudaStream_t stream);
+
+// The kernel's dynamic shared memory, once for each device of the process (a call to the driver otherwise, for every launch).
+template <class Kernel>
+inline bool gen_shared_memory(Kernel* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 
 #ifdef __CUDACC__
 // a sequence's entries, checked: false where one is out of range (one thread of the caller reports it)

@@ -3,8 +3,9 @@
 //
 //     s_j = scale q . k_j    p_j = exp(s_j - m)    o = sum p_j v_j / sum p_j
 //
-// One CTA per (unit, key head): a warp asks for the pages by TMA, 64 tokens a stage; four warps take 16 of the 64 tokens each, so that every
-// key and value is read from shared memory once.  Products are m16n8k16 with tokens (scores) and features (outputs) as m and the rows as n: 8
+// A CTA works off a list of units for one key head; the lists are of the same length in tiles of 64 tokens, as many as the GPU holds CTAs, and a
+// unit that crosses a list's end is cut there.  A warp asks for the pages by TMA, a tile a stage, ahead into the next unit; four warps
+// take 16 of a tile's tokens each, so that every key and value is read from shared memory once.  Products are m16n8k16 with tokens (scores) and features (outputs) as m and the rows as n: 8
 // or 16 rows cost what they are, and fragments let a warp keep scores, softmax and sums in registers.  At so few rows a token the
 // work is far below any tensor path's rate.  A warp has its own running maximum (raised in steps of 2^8 and more), sum and output;
 // the four are joined at the unit's end.
@@ -30,16 +31,17 @@ constexpr int CW = 4, NT = CW * 32 + 32;
 template <bool F8, int NR>             // NR: rows, in eights
 struct Shape {
     // as many CTAs of an SM as registers allow, and stages for what shared memory is left
-    static constexpr int CTAS = NR == 1 ? (F8 ? 4 : 3) : 2, STAGES = NR == 1 ? (F8 ? 3 : 2) : (F8 ? 5 : 3);
+    static constexpr int CTAS = NR == 1 ? 3 : 2, STAGES = NR == 1 ? (F8 ? 4 : 2) : (F8 ? 5 : 3);
     static constexpr int KV = TILE * D * (F8 ? 1 : 2), EXP = F8 ? TILE : 0;
-    // the exponents of a stage lie behind all tiles (which start on 1,024 bytes)
-    static constexpr int exps = STAGES * 2 * KV, misc = exps + STAGES * 2 * EXP, bytes = misc + 256 + 1024;
-    static constexpr int PITCH = D + 4;                       // floats of a row of O where the warps' parts are joined
-    static_assert(CW * 8 * NR * (PITCH + 4) * 4 <= exps, "room for the parts");
+    // the exponents of a stage lie behind all tiles (which start on 1,024 bytes), then half of the warps' outputs for eight rows, to be joined
+    static constexpr int PITCH = D / 2 + 4;
+    static constexpr int exps = STAGES * 2 * KV, joint = exps + STAGES * 2 * EXP, stats = joint + CW * 8 * PITCH * 4, misc = stats + CW * 8 * NR * 16,
+                         bytes = misc + 256 + 1024;
+    static_assert(CTAS * (bytes + 1024) <= 228 * 1024, "shared memory");
 };
 struct Misc {
     uint64_t full[5], empty[5];
-    int dead;
+    int dead, stop;      // latch: a wait ran out; what the four warps have seen of it at a unit's end, all the same
 };
 
 template <bool F16>
@@ -79,8 +81,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     Misc& m = *reinterpret_cast<Misc*>(smem + S::misc);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Unit u = t.units[blockIdx.x / t.Hkv];
-    const int h = blockIdx.x % t.Hkv;
+    const int h = blockIdx.x % t.Hkv, first = t.list_ptr[blockIdx.x / t.Hkv], last = t.list_ptr[blockIdx.x / t.Hkv + 1];
     if (tid == 0) {
         for (int i = 0; i < S::STAGES; i++) {
             mbar_init(&m.full[i], 1);
@@ -89,8 +90,23 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         m.dead = 0;
         fence_barrier_init();
     }
-    // what the unit's rows see: lane i has row i; the farthest token that any sees, and the nearest limit
+    __syncthreads();
     const int g = lane >> 2, c = lane & 3;
+    int st = 0;                                   // the ring of stages runs on over the units
+    uint32_t ph = 0;
+    auto next_stage = [&]() {
+        if (++st == S::STAGES) {
+            st = 0;
+            ph ^= 1;
+        }
+    };
+    bool alive = true;
+#pragma unroll 1
+    for (int item = first; item < last && alive; item++) {
+    const Unit u = t.units[item];
+    const int tile0 = u.k0 & ~(TILE - 1);
+    PageWalk walk(t, u, tile0, warp == CW ? u.k1 : 0);
+    // what the unit's rows see: lane i has row i; the farthest token that any sees, and the nearest limit
     const Row mine = row_of(t, u, min(lane, ROWS - 1), h, q_pos, tid < ROWS ? status : nullptr);
     int far = lane < u.n ? mine.limit : 0, near = lane < u.n ? mine.limit : INT32_MAX;
 #pragma unroll
@@ -98,16 +114,13 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         far = max(far, __shfl_xor_sync(~0u, far, x));
         near = min(near, __shfl_xor_sync(~0u, near, x));
     }
-    const int k1 = min(u.k1, far), tile0 = u.k0 & ~(TILE - 1), n_tiles = k1 > u.k0 ? (k1 - tile0 + TILE - 1) / TILE : 0;
-    __syncthreads();
+    const int k1 = min(u.k1, far), n_tiles = k1 > u.k0 ? (k1 - tile0 + TILE - 1) / TILE : 0;
 
     if (warp == CW) {
         // ---- pages: a box is up to 64 tokens of one page ----------------------------------------------------------------------------
-        PageWalk walk(t, u, tile0, k1);
         const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
-        for (int n = 0; n < n_tiles; n++) {
-            const int st = n % S::STAGES;
-            if (!mbar_wait_warp(&m.empty[st], ((n / S::STAGES) & 1) ^ 1, status, &m.dead)) break;
+        for (int n = 0; n < n_tiles; n++, next_stage()) {
+            if (!(alive = mbar_wait_warp(&m.empty[st], ph ^ 1, status, &m.dead))) break;
             const int j0 = tile0 + n * TILE, boxes = (min(k1 - j0, TILE) + box - 1) >> walk.box_shift;
             unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV, *se = smem + S::exps + st * 2 * S::EXP;
             if (lane == 0) mbar_expect_tx(&m.full[st], boxes * box * (F8 ? 2 * D + 2 : 4 * D));
@@ -178,9 +191,9 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             top[r][0] = top[r][1] = top2[r][0] = top2[r][1] = -INFINITY;
             sum[r][0] = sum[r][1] = 0.f;
         }
-        for (int n = 0; n < n_tiles; n++) {
-            const int st = n % S::STAGES, j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
-            if (!mbar_wait_warp(&m.full[st], (n / S::STAGES) & 1, status, &m.dead)) break;
+        for (int n = 0; n < n_tiles; n++, next_stage()) {
+            const int j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
+            if (!(alive = mbar_wait_warp(&m.full[st], ph, status, &m.dead))) break;
             unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV;
             const unsigned char* se = smem + S::exps + st * 2 * S::EXP + 16 * warp;
             // scores of tokens g and g + 8
@@ -293,7 +306,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             }
             bool bad = false;
             if (edge) {
-                // Behind the last token that any row sees: zeros (this warp's tokens; it is the last tile, nothing is loaded over them).
+                // Behind the last token that any row sees: zeros (this warp's tokens).
                 // Values that some rows see and others do not may be infinite or NaN, and 0 times that is not 0.
                 constexpr int CH = F8 ? 8 : 16;           // 16-byte pieces of a token's values
 #pragma unroll 1
@@ -305,6 +318,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     else bad |= nonfinite<F8>(y.x) || nonfinite<F8>(y.y) || nonfinite<F8>(y.z) || nonfinite<F8>(y.w);
                 }
                 bad = __any_sync(~0u, bad);
+                fence_async_smem();                // (before the next copy into this stage)
                 __syncwarp();
             }
             if (bad) {                             // token by token: what a row does not see adds nothing
@@ -358,67 +372,90 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             if (lane == 0) mbar_arrive(&m.empty[st]);
         }
         // ---- the four warps' parts joined -----------------------------------------------------------------------------------------
-        float* so = reinterpret_cast<float*>(smem);
-        float4* stats = reinterpret_cast<float4*>(so + CW * ROWS * S::PITCH);       // [warp][row]{maximum, sum, what outputs go by, -}
-        asm volatile("bar.sync 1, 128;" ::: "memory");                   // all warps have read all stages
+        float* so = reinterpret_cast<float*>(smem + S::joint);
+        float4* stats = reinterpret_cast<float4*>(smem + S::stats);        // [warp][row]{maximum, sum, what outputs go by, -}
+        constexpr int PER = CW * 4;                                       // threads a row
 #pragma unroll
-        for (int r = 0; r < NR; r++)
+        for (int r8 = 0; r8 < NR; r8++)
 #pragma unroll
             for (int y = 0; y < 2; y++) {
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) sum[r][y] += __shfl_xor_sync(~0u, sum[r][y], x);
-                float* dst = so + (warp * ROWS + 8 * r + 2 * c + y) * S::PITCH;
-#pragma unroll
-                for (int j = 0; j < 8; j++)
-#pragma unroll
-                    for (int x = 0; x < 2; x++) dst[F8 ? 16 * g + 2 * j + x : 16 * j + g + 8 * x] = acc[r][j][2 * x + y];
-                if (g == 0) stats[warp * ROWS + 8 * r + 2 * c + y] = make_float4(top[r][y], sum[r][y], F8 ? top2[r][y] : top[r][y], 0.f);
+                for (int x = 4; x < 32; x <<= 1) sum[r8][y] += __shfl_xor_sync(~0u, sum[r8][y], x);
+                if (g == 0) stats[warp * ROWS + 8 * r8 + 2 * c + y] = make_float4(top[r8][y], sum[r8][y], F8 ? top2[r8][y] : top[r8][y], 0.f);
             }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        constexpr int PER = CW * 32 / ROWS;                               // threads a row
-        const int i = tid / PER;
-        const Row r = row_of(t, u, i, h, q_pos, nullptr);
-        if (i < u.n) {
-            float w[CW], M = -INFINITY, L = 0.f;
 #pragma unroll
-            for (int x = 0; x < CW; x++) M = fmaxf(M, stats[x * ROWS + i].x);
-#pragma unroll
-            for (int x = 0; x < CW; x++) {
-                const float4 y = stats[x * ROWS + i];
-                L += y.x == -INFINITY ? 0.f * y.y : ex2(y.x - M) * y.y;
-                // a warp's output is in units of 2^top2; without a number there, though it has seen something: NaN
-                w[x] = y.y == 0.f ? 0.f : y.z == -INFINITY ? __uint_as_float(0x7fffffffu) : ex2(y.z - M);
-            }
-            const bool none = M == -INFINITY && L == 0.f;
-            const float inv = none ? 0.f : 1.f / L;
+        for (int r8 = 0; r8 < NR; r8++) {
+            if (8 * r8 >= u.n) break;
+            const int i = 8 * r8 + tid / PER;
+            const Row r = row_of(t, u, i, h, q_pos, nullptr);
             const int64_t out = (int64_t)r.row * t.Hq + r.head, part = (int64_t)(u.part0 + u.flat0 + i) * t.Hkv + h;
+            float w[CW], inv = 0.f;
+            bool none = true;
 #pragma unroll
-            for (int e = tid % PER * 4; e < D; e += PER * 4) {
-                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!none)
+            for (int half = 0; half < 2; half++) {
 #pragma unroll
-                    for (int x = 0; x < CW; x++) {
-                        if (w[x] == 0.f) continue;
-                        const float4 z = *reinterpret_cast<const float4*>(so + (x * ROWS + i) * S::PITCH + e);
-                        y.x += w[x] * z.x;
-                        y.y += w[x] * z.y;
-                        y.z += w[x] * z.z;
-                        y.w += w[x] * z.w;
+                for (int y = 0; y < 2; y++) {
+                    float* dst = so + (warp * 8 + 2 * c + y) * S::PITCH;
+                    if constexpr (F8) {
+                        if ((g >> 2) == half)
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+                                *reinterpret_cast<float2*>(dst + 16 * (g & 3) + 2 * j) = make_float2(acc[r8][j][y], acc[r8][j][2 + y]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+#pragma unroll
+                            for (int x = 0; x < 2; x++) dst[16 * j + g + 8 * x] = acc[r8][4 * half + j][2 * x + y];
                     }
-                y.x *= inv;
-                y.y *= inv;
-                y.z *= inv;
-                y.w *= inv;
-                if (r.alone) *reinterpret_cast<uint2*>(o + out * D + e) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-                else *reinterpret_cast<float4*>(part_o + part * D + e) = y;
-            }
-            if (tid % PER == 0) {
-                const float l2 = none ? -INFINITY : M + log2f(L);
-                if (r.alone) lse[out] = l2 * LN2;
-                else part_lse[part] = l2;
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (i < u.n) {
+                    if (half == 0) {
+                        float M = -INFINITY, L = 0.f;
+#pragma unroll
+                        for (int x = 0; x < CW; x++) M = fmaxf(M, stats[x * ROWS + i].x);
+#pragma unroll
+                        for (int x = 0; x < CW; x++) {
+                            const float4 y = stats[x * ROWS + i];
+                            L += y.x == -INFINITY ? 0.f * y.y : ex2(y.x - M) * y.y;
+                            // a warp's output is in units of 2^top2; without a number there, though it has seen something: NaN
+                            w[x] = y.y == 0.f ? 0.f : y.z == -INFINITY ? __uint_as_float(0x7fffffffu) : ex2(y.z - M);
+                        }
+                        none = M == -INFINITY && L == 0.f;
+                        inv = none ? 0.f : 1.f / L;
+                        if (tid % PER == 0) {
+                            const float l2 = none ? -INFINITY : M + log2f(L);
+                            if (r.alone) lse[out] = l2 * LN2;
+                            else part_lse[part] = l2;
+                        }
+                    }
+                    const int e = tid % PER * 4;
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (!none)
+#pragma unroll
+                        for (int x = 0; x < CW; x++) {
+                            if (w[x] == 0.f) continue;
+                            const float4 z = *reinterpret_cast<const float4*>(so + (x * 8 + tid / PER) * S::PITCH + e);
+                            y.x += w[x] * z.x;
+                            y.y += w[x] * z.y;
+                            y.z += w[x] * z.z;
+                            y.w += w[x] * z.w;
+                        }
+                    y.x *= inv;
+                    y.y *= inv;
+                    y.z *= inv;
+                    y.w *= inv;
+                    if (r.alone) *reinterpret_cast<uint2*>(o + out * D + half * 64 + e) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+                    else *reinterpret_cast<float4*>(part_o + part * D + half * 64 + e) = y;
+                }
+                if (tid == 0) m.stop = *reinterpret_cast<volatile int*>(&m.dead);
+                asm volatile("bar.sync 1, 128;" ::: "memory");           // it has been read
             }
         }
+        alive = *reinterpret_cast<volatile int*>(&m.stop) == 0;
     }
+    }
+    let_next_launch();
     if (__syncthreads_or(m.dead)) drain_delay();          // abandoned: copies in flight must land before the CTA goes
     after_previous();                                     // (the wide kernel ran beside this one; the merge waits for this one only)
 }
@@ -427,56 +464,68 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
 constexpr int MERGE_WARPS = 4;
 __global__ void __launch_bounds__(MERGE_WARPS * 32)
 merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __restrict__ part_lse, __nv_bfloat16* __restrict__ o, float* __restrict__ lse) {
-    after_previous();
     const int64_t out = (int64_t)blockIdx.x * MERGE_WARPS + (threadIdx.x >> 5);
-    if (out >= (int64_t)t.n_q * t.Hq) return;
+    if (out >= (int64_t)t.n_q * t.Hq) {
+        after_previous();
+        return;
+    }
     const int lane = threadIdx.x & 31, row = (int)(out / t.Hq), head = (int)(out % t.Hq), G = t.Hq / t.Hkv, h = head / G, g = head % G;
+    // (the index is the call's input: only the parts are the previous kernels')
     const int p0 = t.part_ptr[row], p1 = t.part_ptr[row + 1];
+    int at = p0 + lane < p1 ? t.part[p0 + lane] + g : -1;
+    after_previous();
     if (p1 == p0 + 1) return;
     float M = -INFINITY, L = 0.f;
-    bool nan = false;
-    for (int p = p0 + lane; p < p1; p += 32) {
-        const float y = part_lse[(int64_t)(t.part[p] + g) * t.Hkv + h];
-        M = fmaxf(M, y);
-        nan |= y != y;
-    }
-#pragma unroll
-    for (int x = 1; x < 32; x <<= 1) M = fmaxf(M, __shfl_xor_sync(~0u, M, x));
-    nan = __any_sync(~0u, nan);
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (M > -INFINITY || nan) {
-#pragma unroll 4
-        for (int p = p0; p < p1; p++) {
-            const int64_t at = (int64_t)(t.part[p] + g) * t.Hkv + h;
-            const float w = ex2(part_lse[at] - M);
-            const float4 z = *reinterpret_cast<const float4*>(part_o + at * D + 4 * lane);
-            if (w == 0.f) continue;
-            L += w;
-            y.x += w * z.x;
-            y.y += w * z.y;
-            y.z += w * z.z;
-            y.w += w * z.w;
+    bool nan = false;
+    for (int b = p0; b < p1; b += 32) {           // 32 parts at a time: a lane has a part's place and weight
+        const int n = min(32, p1 - b);
+        if (b > p0) at = lane < n ? t.part[b + lane] + g : -1;
+        const float l = lane < n ? part_lse[(int64_t)at * t.Hkv + h] : -INFINITY;
+        nan |= l != l;
+        float m = l;
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, x));
+        if (m > M) {
+            const float f = ex2(M - m);           // from -inf: 0, and all sums are 0
+            L *= f;
+            y.x *= f;
+            y.y *= f;
+            y.z *= f;
+            y.w *= f;
+            M = m;
         }
-        const float inv = 1.f / L;
-        y.x *= inv;
-        y.y *= inv;
-        y.z *= inv;
-        y.w *= inv;
+        const float w = M == -INFINITY ? 0.f : ex2(l - M);
+#pragma unroll 8
+        for (int i = 0; i < n; i++) {
+            const float wi = __shfl_sync(~0u, w, i);
+            const float4 z = *reinterpret_cast<const float4*>(part_o + ((int64_t)__shfl_sync(~0u, at, i) * t.Hkv + h) * D + 4 * lane);
+            L += wi;
+            if (wi == 0.f) continue;              // (0 times an infinity is not 0)
+            y.x += wi * z.x;
+            y.y += wi * z.y;
+            y.z += wi * z.z;
+            y.w += wi * z.w;
+        }
     }
-    *reinterpret_cast<uint2*>(o + out * D + 4 * lane) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-    if (lane == 0) lse[out] = M == -INFINITY && !nan ? -INFINITY : (M + log2f(L)) * LN2;
+    nan = __any_sync(~0u, nan);
+    const bool none = M == -INFINITY && !nan;
+    const float inv = none ? 0.f : nan ? __uint_as_float(0x7fffffffu) : 1.f / L;
+    *reinterpret_cast<uint2*>(o + out * D + 4 * lane) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
+    if (lane == 0) lse[out] = none ? -INFINITY : nan ? inv : (M + log2f(L)) * LN2;
 }
 
 template <bool F8, int NR>
-int32_t launch_narrow(const Tables& t, int n_units, const Call& a, bool follows) {
+int32_t launch_narrow(const Tables& t, int n_lists, const Call& a, bool follows) {
     using S = Shape<F8, NR>;
-    if (cudaFuncSetAttribute(narrow_kernel<F8, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    static std::atomic<uint64_t> set{0};
+    if (!gen_shared_memory(narrow_kernel<F8, NR>, S::bytes, set)) return HARTS_ECUDA;
     const auto *q = static_cast<const __nv_bfloat16*>(a.q);
     auto* o = static_cast<__nv_bfloat16*>(a.o);
     if (follows)
-        return launch_after(narrow_kernel<F8, NR>, n_units * t.Hkv, NT, S::bytes, a.stream, t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp,
+        return launch_after(narrow_kernel<F8, NR>, n_lists * t.Hkv, NT, S::bytes, a.stream, t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp,
                             a.q_pos, a.scale_log2, o, a.lse, a.part_o, a.part_lse, a.dev_status) == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
-    narrow_kernel<F8, NR><<<n_units * t.Hkv, NT, S::bytes, a.stream>>>(t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp, a.q_pos, a.scale_log2, o,
+    narrow_kernel<F8, NR><<<n_lists * t.Hkv, NT, S::bytes, a.stream>>>(t, q, a.ld_q, a.map_k, a.map_v, a.cache.k_exp, a.cache.v_exp, a.q_pos, a.scale_log2, o,
                                                                       a.lse, a.part_o, a.part_lse, a.dev_status);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
@@ -511,7 +560,8 @@ int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int
     if (hi[N_NARROW] > 0) {
         t.units = reinterpret_cast<const Unit*>(di + hi[NARROW]);
         auto* narrow = hi[NARROW_MAX] <= 8 ? (f8 ? launch_narrow<true, 1> : launch_narrow<false, 1>) : (f8 ? launch_narrow<true, 2> : launch_narrow<false, 2>);
-        if ((rc = narrow(t, hi[N_NARROW], a, hi[N_WIDE] > 0)) != HARTS_OK) return rc;
+        t.list_ptr = di + hi[LIST_PTR];
+        if ((rc = narrow(t, hi[N_LISTS], a, hi[N_WIDE] > 0)) != HARTS_OK) return rc;
     }
     if (hi[MERGED]) {
         const int64_t blocks = ((int64_t)t.n_q * t.Hq + MERGE_WARPS - 1) / MERGE_WARPS;

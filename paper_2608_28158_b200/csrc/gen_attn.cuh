@@ -20,7 +20,7 @@ constexpr float RAISE = 8.f;            // a running maximum follows in steps of
 struct Tables {
     const Unit* units;
     const Entry* entries;
-    const int32_t *pages, *part_ptr, *part;
+    const int32_t *pages, *part_ptr, *part, *list_ptr;
     int n_q, Hq, Hkv, page;
 };
 // Row i of a unit: its query and the query head; what it sees ends at `limit`.

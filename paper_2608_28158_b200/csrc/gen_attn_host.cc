@@ -17,8 +17,15 @@ using namespace harts::gen_attn;
 
 constexpr int TILE = 64;
 constexpr int MIXED = 2 * TILE;         // limits this near to each other share a run
-constexpr int LEAST = 256;              // tokens a unit is not cut below
-constexpr int CTAS = 148 * 3;           // units wanted, all key heads together
+constexpr int LEAST = 256;              // tokens a wide unit is not cut below
+// CTAs wanted, all key heads together: as many as the GPU holds.  Of the wide kernel three quarters of that: what is left lets the narrow one
+// start beside it (64 branches of a prompt of 16,421 tokens 84 -> 78 us).
+constexpr int SMS = 148, WIDE_CTAS = SMS * 3 / 2;
+constexpr int PIECE = 2;                // tiles that a unit costs besides its own, and that are not cut off one
+// Below so many tokens (one short unit an SM, all key heads) a call's time is the kernels' latency, and the narrow kernel's is the shorter:
+// 28 rows x 700 tokens 12.4 against 16.4 us.  Above, from 16 rows on the wide one (agentic trees, 32 rows x 900: 92 against 119 us).
+constexpr int64_t SMALL = SMS * 256;
+constexpr int SMALL_ROWS = 32;
 
 struct Range {
     int node, a, b, entry, n_entries;
@@ -27,7 +34,7 @@ struct Range {
 struct Index {
     std::vector<Unit> narrow, wide;
     std::vector<Entry> entries;
-    std::vector<int32_t> part_ptr, part;
+    std::vector<int32_t> part_ptr, part, list_ptr;
     int32_t n_parts = 0, merged = 0, max_page = -1;
 };
 
@@ -63,11 +70,14 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
         for (; parent[v] >= 0; v = base[v] + parent[v])
             if (off[v] > 0) sees[base[v] + parent[v]].push_back({r, off[v]});
     }
+    int64_t tokens = 0;
+    for (int32_t v = 0; v < n_nodes; v++) tokens += sees[v].empty() ? 0 : len[v];
+    const int64_t most_rows = tokens * Hkv < SMALL ? SMALL_ROWS : NARROW_ROWS;
     std::vector<Range> ranges;
     std::vector<int32_t> parts_of(n_q, 0);
     auto add = [&](int node, int a, int b, bool wide, const std::vector<Entry>& e) {
         if (e.empty() || b <= a) return;
-        ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), wide && (int64_t)e.size() * G > NARROW_ROWS});
+        ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), wide && (int64_t)e.size() * G > most_rows});
         ix.entries.insert(ix.entries.end(), e.begin(), e.end());
     };
     std::vector<Entry> e;
@@ -122,39 +132,116 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
         if (n_own) {
             e.clear();
             for (const Sees& x : s)
-                if (x.limit < 0) e.push_back({x.row, -1, own_from, (int32_t)most});
+                if (x.limit < 0) e.push_back({x.row, -1, q_pos[x.row] + 1, (int32_t)most});
             add(v, own_from, (int)most, false, e);
         }
     }
-    // cut long runs: as many units as keep the GPU busy, none shorter than LEAST
-    int64_t total = 0;
-    auto units_of = [&](const Range& r) {
-        const int64_t rows = (int64_t)r.n_entries * G;
-        return (rows + (r.wide ? WIDE_ROWS : NARROW_ROWS) - 1) / (r.wide ? WIDE_ROWS : NARROW_ROWS);
-    };
-    for (const Range& r : ranges) total += units_of(r) * (r.b - r.a) * Hkv;
-    const int64_t cut = std::max<int64_t>(LEAST, (total + CTAS - 1) / CTAS);
     std::stable_sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.b - x.a > y.b - y.a; });
     std::vector<std::vector<int32_t>> parts(n_q);
     int64_t n_parts = 0;
+    // queries first_entry .. + n of a range, for tokens k0 .. k1, in blocks of `per` rows
+    auto put = [&](std::vector<Unit>& to, const Range& r, int first_entry, int n, int per, int k0, int k1) {
+        const int rows = n * G;
+        for (int f = 0; f < rows; f += per)
+            to.push_back({r.entry + first_entry, f, std::min(per, rows - f), k0, k1, page_ptr[r.node], (int32_t)n_parts, 0});
+        for (int i = 0; i < n; i++) parts[ix.entries[r.entry + first_entry + i].row].push_back((int32_t)(n_parts + (int64_t)i * G));
+        n_parts += rows;
+        return n_parts <= INT32_MAX - (1 << 20);
+    };
+
+    // The wide kernel's runs: the shortest pieces that still make one wave; with more units than that anyway, pieces of half a CTA's share.
+    int64_t total = 0, units = 0, lo = LEAST, hi = LEAST;
+    auto blocks = [&](const Range& r) { return ((int64_t)r.n_entries * G + WIDE_ROWS - 1) / WIDE_ROWS; };
+    for (const Range& r : ranges)
+        if (r.wide) {
+            total += blocks(r) * (r.b - r.a) * Hkv;
+            units += blocks(r) * Hkv;
+            hi = std::max<int64_t>(hi, r.b - r.a);
+        }
+    if (units > WIDE_CTAS) lo = hi = std::max<int64_t>(LEAST, total / (2 * WIDE_CTAS));
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        int64_t n = 0;
+        for (const Range& r : ranges)
+            if (r.wide) n += blocks(r) * Hkv * ((r.b - r.a + mid - 1) / mid);
+        if (n <= WIDE_CTAS) hi = mid;
+        else lo = mid + 1;
+    }
     for (const Range& r : ranges) {
-        const int64_t n = r.b - r.a, rows = (int64_t)r.n_entries * G, per = r.wide ? WIDE_ROWS : NARROW_ROWS;
-        const int64_t pieces = (n + cut - 1) / cut;
+        if (!r.wide) continue;
+        const int64_t n = r.b - r.a, pieces = (n + lo - 1) / lo;
         for (int64_t p = 0; p < pieces; p++) {
             auto edge = [&](int64_t i) { return (int32_t)(i <= 0 ? r.a : i >= pieces ? r.b : std::max<int64_t>(r.a, (r.a + n * i / pieces) / TILE * TILE)); };
-            const int32_t k0 = edge(p), k1 = edge(p + 1);
-            if (k1 <= k0) continue;
-            for (int64_t f = 0; f < rows; f += per)
-                (r.wide ? ix.wide : ix.narrow).push_back({r.entry, (int32_t)f, (int32_t)std::min(per, rows - f), k0, k1, page_ptr[r.node], (int32_t)n_parts, 0});
-            for (int i = 0; i < r.n_entries; i++) parts[ix.entries[r.entry + i].row].push_back((int32_t)(n_parts + (int64_t)i * G));
-            n_parts += rows;
-            if (n_parts > INT32_MAX - (1 << 20)) return HARTS_EINVAL;
+            if (edge(p + 1) > edge(p) && !put(ix.wide, r, 0, r.n_entries, WIDE_ROWS, edge(p), edge(p + 1))) return HARTS_EINVAL;
         }
     }
+    std::stable_sort(ix.wide.begin(), ix.wide.end(), [](const Unit& x, const Unit& y) { return x.k1 - x.k0 > y.k1 - y.k0; });
+
+    // The narrow kernel's: queries in blocks of 16 rows (a query of more heads is several blocks that are cut alike), and a list for every CTA
+    // until its share of the tiles is full; a run that crosses a list's end is cut there.
+    const int per_block = std::max(1, NARROW_ROWS / G);
+    int64_t tiles = 0, strips = 0;
+    int most = 0;                                  // rows of a unit
+    const int chunks = (G + NARROW_ROWS - 1) / NARROW_ROWS;
+    auto tiles_of = [](int a, int b) { return (int64_t)(b + TILE - 1) / TILE - a / TILE; };
+    for (const Range& r : ranges)
+        if (!r.wide) {
+            const int64_t n = (r.n_entries + per_block - 1) / per_block * (int64_t)chunks;
+            strips += n;
+            tiles += n * tiles_of(r.a, r.b);
+            most = std::max(most, std::min(r.n_entries * G, std::min(per_block * G, NARROW_ROWS)));
+        }
+    if (strips) {
+        const int64_t ctas = SMS * (most <= 8 ? 3 : 2), lists = std::max<int64_t>(1, ctas / Hkv);
+        // the lists for a share of tiles: piece(range, first query, queries, from, to) and closed() in order; how many there are
+        auto fill = [&](int64_t share, auto piece, auto closed) {
+            int64_t full = 0, n_lists = 0;        // full: tiles of the list that is being filled
+            auto close = [&]() {
+                if (full > 0) {
+                    closed();
+                    n_lists++;
+                }
+                full = 0;
+            };
+            for (const Range& r : ranges) {
+                if (r.wide) continue;
+                for (int e0 = 0; e0 < r.n_entries; e0 += per_block) {
+                    const int n = std::min(per_block, r.n_entries - e0);
+                    for (int a = r.a; a < r.b;) {
+                        int64_t take = (share - full - PIECE) / chunks;
+                        const int64_t left = tiles_of(a, r.b);
+                        if (full > 0 && take < std::min<int64_t>(left, PIECE)) {
+                            close();
+                            take = (share - PIECE) / chunks;
+                        }
+                        take = std::max<int64_t>(take, 1);
+                        const int b = left <= take ? r.b : (int)((a / TILE + take) * TILE);
+                        piece(r, e0, n, a, b);
+                        full += chunks * (tiles_of(a, b) + PIECE);
+                        a = b;
+                    }
+                }
+            }
+            close();
+            return n_lists;
+        };
+        // the smallest share that needs no more lists than there are CTAs
+        auto none = [](auto&&...) {};
+        int64_t lo = std::max<int64_t>((tiles + strips * PIECE) / lists, 2 * PIECE), hi = lo;
+        while (fill(hi, none, none) > lists) hi += hi / 4 + 1;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (fill(mid, none, none) <= lists) hi = mid;
+            else lo = mid + 1;
+        }
+        bool fits = true;
+        ix.list_ptr.assign(1, 0);
+        fill(lo,
+             [&](const Range& r, int e0, int n, int a, int b) { fits = put(ix.narrow, r, e0, n, chunks > 1 ? NARROW_ROWS : n * G, a, b) && fits; },
+             [&]() { ix.list_ptr.push_back((int32_t)ix.narrow.size()); });
+        if (!fits) return HARTS_EINVAL;
+    }
     ix.n_parts = (int32_t)n_parts;
-    auto longer = [](const Unit& x, const Unit& y) { return x.k1 - x.k0 > y.k1 - y.k0; };
-    std::stable_sort(ix.narrow.begin(), ix.narrow.end(), longer);
-    std::stable_sort(ix.wide.begin(), ix.wide.end(), longer);
     ix.part_ptr.assign(1, 0);
     for (int32_t r = 0; r < n_q; r++) {
         if (parts[r].size() == 1) parts[r][0] = -1;               // written by its unit
@@ -187,10 +274,10 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
                                  grow, ix);
         if (rc != HARTS_OK) return rc;
         const int64_t n_pages = node_page_ptr[tree_node_ptr[n_trees]];
-        int64_t total = HARTS_GEN_ATTN_HEADER_WORDS, at[6];
-        const int64_t sizes[6] = {(int64_t)(ix.narrow.size() * sizeof(Unit) / 4), (int64_t)(ix.wide.size() * sizeof(Unit) / 4),
-                                  (int64_t)(ix.entries.size() * sizeof(Entry) / 4), n_pages, n_q + 1, (int64_t)ix.part.size()};
-        for (int i = 0; i < 6; i++) {
+        int64_t total = HARTS_GEN_ATTN_HEADER_WORDS, at[7];
+        const int64_t sizes[7] = {(int64_t)(ix.narrow.size() * sizeof(Unit) / 4), (int64_t)(ix.wide.size() * sizeof(Unit) / 4),
+                                  (int64_t)(ix.entries.size() * sizeof(Entry) / 4), n_pages, n_q + 1, (int64_t)ix.part.size(), (int64_t)ix.list_ptr.size()};
+        for (int i = 0; i < 7; i++) {
             at[i] = total;
             total += (sizes[i] + 3) & ~int64_t(3);            // 16-byte aligned starts
         }
@@ -211,6 +298,8 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
         blob[WORDS] = (int32_t)total;
         for (const Unit& u : ix.narrow) blob[NARROW_MAX] = std::max(blob[NARROW_MAX], u.n);
         for (int i = 0; i < 6; i++) blob[NARROW + i] = (int32_t)at[i];
+        blob[N_LISTS] = std::max<int32_t>(0, (int32_t)ix.list_ptr.size() - 1);
+        blob[LIST_PTR] = (int32_t)at[6];
         auto put = [&](int i, const void* p, int64_t words) {
             if (words) std::copy_n(static_cast<const int32_t*>(p), words, blob + at[i]);
         };
@@ -220,6 +309,7 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
         put(3, node_page, sizes[3]);
         put(4, ix.part_ptr.data(), sizes[4]);
         put(5, ix.part.data(), sizes[5]);
+        put(6, ix.list_ptr.data(), sizes[6]);
     } catch (const std::bad_alloc&) {
         return HARTS_ENOMEM;
     } catch (...) {

@@ -35,12 +35,12 @@ struct Shape {
 };
 constexpr int COL_S = 0, COL_O = 128, TMEM_COLS = 256;     // S / P of tile n at COL_S + 64 (n & 1)
 struct Misc {
-    uint64_t k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, kp_full[2];      // 8 bits: k, kfree are those of the stages of pages
+    uint64_t q, k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, kp_full[2];      // 8 bits: k, kfree are those of the stages of pages
     int dead;
     uint32_t tmem;
-    float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: powers of a tile's keys, and what makes a row's score log2 units
+    alignas(16) float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: powers of a tile's keys, and what makes a row's score log2 units
 };
-static_assert(offsetof(Misc, kp) <= 256 && sizeof(Misc) <= 1280, "misc area");
+static_assert(offsetof(Misc, kp) <= 256 && offsetof(Misc, kp) % 16 == 0 && sizeof(Misc) <= 1280 && Shape<true>::misc % 16 == 0, "misc area");
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
@@ -88,6 +88,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             const int32_t* __restrict__ q_pos, float scale_log2, __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ part_o,
             float* __restrict__ part_lse, int* status) {
     using S = Shape<F8>;
+    constexpr int Q_WARPS = F8 ? 8 : 4;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     Misc& m = *reinterpret_cast<Misc*>(smem + S::misc);
@@ -106,6 +107,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             mbar_init(&m.p[i], active);
             mbar_init(&m.kp_full[i], 2);
         }
+        mbar_init(&m.q, Q_WARPS);
         mbar_init(&m.pv, 1);
         mbar_init(&m.o, 1);
         mbar_init(&m.exit, 1);
@@ -113,49 +115,53 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         fence_barrier_init();
     }
     if (warp == 0) tmem_alloc<TMEM_COLS>(&m.tmem);
-    // the rows' queries, half a warp a row
-    for (int i = tid >> 4; i < WIDE_ROWS; i += S::NT / 16) {
-        const int ch = tid & 15;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (i < u.n) {
-            const int G = t.Hq / t.Hkv, flat = u.flat0 + i;
-            x = *reinterpret_cast<const uint4*>(q + (int64_t)t.entries[u.entry + flat / G].row * ld_q + (int64_t)(h * G + flat % G) * D + ch * 8);
-        }
-        if constexpr (F8) {
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            uint32_t top = 0, hi[2] = {0, 0}, lo[2] = {0, 0};
-#pragma unroll
-            for (int e = 0; e < 4; e++) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
-            top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
-            const PowerOfTwo f(top, 7);
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const float2 y = f.apply(w[e]);
-                const uint32_t y8 = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
-                const uint32_t y16 = widen(y8);
-                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&y16));
-                hi[e >> 1] |= y8 << (16 * (e & 1));
-                lo[e >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y.x - back.x, y.y - back.y), __NV_SATFINITE, __NV_E4M3) << (16 * (e & 1));
-            }
-            unsigned char* dst = smem + S::q + sw128_chunk(i, ch >> 1) + 8 * (ch & 1);
-            *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
-            *reinterpret_cast<uint2*>(dst + S::Q_BYTES / 2) = make_uint2(lo[0], lo[1]);
-            if (ch == 0) m.f[i] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : f.undone(scale_log2);      // infinite or NaN: NaN
-        } else {
-            *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
-        }
-    }
-    fence_async_smem();
+    PageWalk walk(t, u, tile0, warp == NS / 32 + 1 ? u.k1 : 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = m.tmem;
+    if (warp < NS / 32 || warp >= NS / 32 + 2) {
+        // the rows' queries, half a warp a row, while the first pages are on their way
+        for (int i = (warp < NS / 32 ? tid : tid - 64) >> 4; i < WIDE_ROWS; i += Q_WARPS * 2) {
+            const int ch = tid & 15;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (i < u.n) {
+                const int G = t.Hq / t.Hkv, flat = u.flat0 + i;
+                x = *reinterpret_cast<const uint4*>(q + (int64_t)t.entries[u.entry + flat / G].row * ld_q + (int64_t)(h * G + flat % G) * D + ch * 8);
+            }
+            if constexpr (F8) {
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                uint32_t top = 0, hi[2] = {0, 0}, lo[2] = {0, 0};
+    #pragma unroll
+                for (int e = 0; e < 4; e++) top = __vmaxu2(top, w[e] & 0x7fff7fffu);
+                top = max(top & 0xffffu, top >> 16);
+    #pragma unroll
+                for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+                const PowerOfTwo f(top, 7);
+    #pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float2 y = f.apply(w[e]);
+                    const uint32_t y8 = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
+                    const uint32_t y16 = widen(y8);
+                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&y16));
+                    hi[e >> 1] |= y8 << (16 * (e & 1));
+                    lo[e >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(y.x - back.x, y.y - back.y), __NV_SATFINITE, __NV_E4M3) << (16 * (e & 1));
+                }
+                unsigned char* dst = smem + S::q + sw128_chunk(i, ch >> 1) + 8 * (ch & 1);
+                *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
+                *reinterpret_cast<uint2*>(dst + S::Q_BYTES / 2) = make_uint2(lo[0], lo[1]);
+                if (ch == 0) m.f[i] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : f.undone(scale_log2);      // infinite or NaN: NaN
+            } else {
+                *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
+            }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m.q);
+    }
 
     if (warp == NS / 32 + 1) {
         // ---- pages ---------------------------------------------------------------------------------------------------------------------
-        PageWalk walk(t, u, tile0, u.k1);
         const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
         for (int n = 0; n < n_tiles; n++) {
             const int st = n & 1, ph = ((n >> 1) & 1) ^ 1;
@@ -224,7 +230,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             __syncwarp();
             return true;
         };
-        bool alive = issue_s(0);
+        bool alive = mbar_wait_warp(&m.q, 0, status, &m.dead) && issue_s(0);
         for (int n = 0; n < n_tiles && alive; n++) {
             const int st = n & 1, steps = (valid(n) + 15) >> 4;
             // S of tile n + 1 goes to the other buffer and runs under the softmax of tile n (that buffer's P was read by the P V
@@ -291,6 +297,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
     } else if (warp < active) {
         // ---- softmax: a row per thread -----------------------------------------------------------------------------------------------------
         const uint32_t tm_lane = tmem + ((uint32_t)(warp * 32) << 16);
+        if (F8) mbar_wait_warp(&m.q, 0, status, &m.dead);         // (the rows' factors are other warps')
         const float scale = F8 ? m.f[tid] : scale_log2;
         const F2 scale2 = f2(scale, scale);
         float m_ref = -INFINITY, l_sum = 0.f;
@@ -426,7 +433,8 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
 template <bool F8>
 int32_t launch(const Tables& t, int n_units, const Call& a) {
     using S = Shape<F8>;
-    if (cudaFuncSetAttribute(wide_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    static std::atomic<uint64_t> set{0};
+    if (!gen_shared_memory(wide_kernel<F8>, S::bytes, set)) return HARTS_ECUDA;
     wide_kernel<F8><<<n_units * t.Hkv, S::NT, S::bytes, a.stream>>>(t, static_cast<const __nv_bfloat16*>(a.q), a.ld_q, a.map_k, a.map_v, a.cache.k_exp,
                                                                   a.cache.v_exp, a.q_pos, a.scale_log2, static_cast<__nv_bfloat16*>(a.o), a.lse, a.part_o,
                                                                   a.part_lse, a.dev_status);

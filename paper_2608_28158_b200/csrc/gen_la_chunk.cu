@@ -315,7 +315,8 @@ int32_t gen_la_chunks(const GenLaArgs& a) {
         int32_t rc;
         if ((rc = make_row_map_ld(&mk, a.k, a.n_rows, a.H, a.ld_k)) != HARTS_OK) return rc;
         if ((rc = make_row_map_ld(&mv, a.v, a.n_rows, a.H, a.ld_v)) != HARTS_OK) return rc;
-        if (cudaFuncSetAttribute(sum_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SUM_BYTES) != cudaSuccess) return HARTS_ECUDA;
+        static std::atomic<uint64_t> set{0};
+        if (!gen_shared_memory(sum_kernel, SUM_BYTES, set)) return HARTS_ECUDA;
         if (launch_after(sum_kernel, (int)(z.max_items * a.H), SUM_THREADS, SUM_BYTES, a.stream, mk, mv, a.g, a.H, gen, (const int*)follows, gamma,
                          a.dev_status) != cudaSuccess)
             return HARTS_ECUDA;

@@ -926,7 +926,8 @@ int32_t launch_gen(const GenLaArgs& a, const GenItems& items, int64_t max_items)
     if ((rc = make_row_map_ld(&mk, a.k, rows, a.H, a.ld_k)) != HARTS_OK) return rc;
     if ((rc = make_row_map_ld(&mv, a.v, rows, a.H, a.ld_v)) != HARTS_OK) return rc;
     if ((rc = make_row_map(&mo, a.o ? a.o : a.k, rows, a.H)) != HARTS_OK) return rc;
-    if (cudaFuncSetAttribute(pipe_fwd_kernel<NV, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::bytes) != cudaSuccess) return HARTS_ECUDA;
+    static std::atomic<uint64_t> set{0};
+    if (!gen_shared_memory(pipe_fwd_kernel<NV, true>, S::bytes, set)) return HARTS_ECUDA;
     const int64_t n = max_items * a.H * (D / NV);
     return launch_after(pipe_fwd_kernel<NV, true>, n < sm_count() ? (int)n : sm_count(), NT, S::bytes, a.stream, harts_la_tables_t{}, items, 0, 0, a.H,
                         mq, mk, mv, mq, mo, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, a.g,

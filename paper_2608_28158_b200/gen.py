@@ -4,13 +4,12 @@ Argument checks here are those that need the tensors' shapes, types, strides and
 with HARTS_EINVAL (HARTS_EUNSUPPORTED for a type or size without a kernel) and launches nothing."""
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 
 import numpy as np
 import torch
 
-from .binding import lib, HartsError, HARTS_BF16, _check, _DTYPE_CODE, _I32P
+from .binding import lib, HartsError, HARTS_BF16, HARTS_OK, _check, _DTYPE_CODE, _I32P
 
 HARTS_E4M3 = 2
 HARTS_EINVAL, HARTS_EUNSUPPORTED = -1, -3
@@ -28,8 +27,18 @@ for _n in ("harts_gen_la_workspace_bytes", "harts_gen_la", "harts_gen_cache_writ
     getattr(lib, _n).restype = _i32
 
 
+# the current stream's handle without the Stream object around it, which costs more than a call's other checks together
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
 def _bad(where, what, code=HARTS_EINVAL):
     raise HartsError(code, f"{where} ({what})")
+
+
+def _bad_tensor(where, name, t, dev):
+    if t.get_device() != dev:
+        _bad(where, f"{name} is on {t.device}" + (f", others on cuda:{dev}" if t.is_cuda else ""))
+    _bad(where, f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
 
 
 def _p(t):
@@ -42,38 +51,57 @@ def _code(where, dtype):
     return _DTYPE_CODE[dtype]
 
 
-def _rows(where, name, t, heads, d, dtype, n=None):
-    """Elements between the rows of a [rows, heads, d] tensor whose heads are contiguous."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or t.dtype != dtype or (n is not None and t.shape[0] != n):
-        _bad(where, f"{name}: {tuple(t.shape)} {t.dtype}")
-    if (d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d):
-        _bad(where, f"{name}: strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
-
-
-def _plain(where, name, t, dtype, shape):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        _bad(where, f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}")
-
-
-def _one_device(where, **tensors):
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            _bad(where, f"{name} is not on a CUDA device")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            _bad(where, f"{name} is on {t.device}, others on {dev}")
+def _device(where, name, t):
+    dev = t.get_device()
+    if dev < 0:
+        _bad(where, f"{name} is not on a CUDA device")
     return dev
 
 
-def _on(dev, stream):
-    """The device made current for the launch, and the stream: the given one or the current one of that device."""
-    guard = contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
-    return guard, (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+def _rows(where, name, t, shape, dtype, dev):
+    """Elements between the rows of a [rows, heads, d] tensor whose heads are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _bad_tensor(where, name, t, dev)
+    rows, heads, d = shape
+    ld, sh, sd = t.stride()
+    if (sd != 1 and d > 1) or (sh != d and heads > 1):
+        _bad_tensor(where, name, t, dev)
+    return ld if rows > 1 else heads * d
+
+
+def _plain(where, name, t, dtype, shape, dev):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        _bad_tensor(where, name, t, dev)
+    return t.data_ptr()
+
+
+def _bytes(where, name, t, dev):
+    """Pointer and size of a work buffer of any type, or of none."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or t.get_device() != dev:
+        _bad_tensor(where, name, t, dev)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _status(where, t, dev):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < 2 or not t.is_contiguous() or t.get_device() != dev:
+        _bad_tensor(where, "dev_status", t, dev)
+    return t.data_ptr()
+
+
+def _call(where, f, dev, stream, *args):
+    """The call on the given stream, or the current one of the tensors' device, with that device current."""
+    st = _raw_stream(dev) if stream is None else stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        code = f(*args, st)
+    else:
+        with torch.cuda.device(dev):
+            code = f(*args, st)
+    if code != HARTS_OK:
+        raise HartsError(code, where)
 
 
 def harts_gen_la_workspace_bytes(n_seq, max_len, n_rows, H, dk, dv, dtype) -> int:
@@ -86,82 +114,67 @@ def harts_gen_la_workspace_bytes(n_seq, max_len, n_rows, H, dk, dv, dtype) -> in
 def harts_gen_la(q, k, v, g, o, states, seq_begin, seq_len, in_state, out_state, max_len, workspace=None, dev_status=None, stream=None):
     """Linear attention from and into kept states (harts_gen.h).  q may be None where o is."""
     w = "harts_gen_la"
-    dev = _one_device(w, k=k, q=q, v=v, g=g, o=o, states=states, seq_begin=seq_begin, seq_len=seq_len, in_state=in_state,
-                      out_state=out_state, workspace=workspace, dev_status=dev_status)
-    if k.dim() != 3:
-        _bad(w, f"k: {tuple(k.shape)}")
-    (rows, H, d), dt, n_seq = k.shape, k.dtype, seq_begin.shape[0] if seq_begin.dim() == 1 else -1
+    dev = _device(w, "k", k)
+    if k.dim() != 3 or states.dim() != 4 or seq_begin.dim() != 1:
+        _bad(w, f"k: {tuple(k.shape)}, states: {tuple(states.shape)}, seq_begin: {tuple(seq_begin.shape)}")
+    shape, dt, n_seq, n_states = k.shape, k.dtype, seq_begin.shape[0], states.shape[0]
+    rows, H, d = shape
     code = _code(w, dt)
-    ld_k, ld_v = _rows(w, "k", k, H, d, dt), _rows(w, "v", v, H, d, dt, rows)
-    ld_q = 0
+    ld_k, ld_v = _rows(w, "k", k, shape, dt, dev), _rows(w, "v", v, shape, dt, dev)
+    ld_q = o_ptr = 0
     if o is not None:
         if q is None:
             _bad(w, "o without q")
-        ld_q = _rows(w, "q", q, H, d, dt, rows)
-        _plain(w, "o", o, dt, (rows, H, d))
-    _plain(w, "g", g, torch.float32, (rows, H))
-    if states.dim() != 4:
-        _bad(w, f"states: {tuple(states.shape)}")
-    _plain(w, "states", states, torch.float32, (states.shape[0], H, d, d))
-    for name, t in (("seq_begin", seq_begin), ("seq_len", seq_len), ("in_state", in_state), ("out_state", out_state)):
-        _plain(w, name, t, torch.int32, (n_seq,))
-    if workspace is not None and not workspace.is_contiguous():
-        _bad(w, "workspace is not contiguous")
-    guard, st = _on(dev, stream)
-    with guard:
-        _check(lib.harts_gen_la(n_seq, _p(seq_begin), _p(seq_len), _p(in_state), _p(out_state), max_len, rows, _p(q), ld_q, _p(k), ld_k,
-                                _p(v), ld_v, _p(g), _p(o), _p(states), states.shape[0], H, d, d, code, _p(workspace),
-                                0 if workspace is None else workspace.numel() * workspace.element_size(), _p(dev_status), st), w)
+        ld_q = _rows(w, "q", q, shape, dt, dev)
+        o_ptr = _plain(w, "o", o, dt, shape, dev)
+    i32, one = torch.int32, (n_seq,)
+    ws, ws_bytes = _bytes(w, "workspace", workspace, dev)
+    _call(w, lib.harts_gen_la, dev, stream, n_seq, _plain(w, "seq_begin", seq_begin, i32, one, dev), _plain(w, "seq_len", seq_len, i32, one, dev),
+          _plain(w, "in_state", in_state, i32, one, dev), _plain(w, "out_state", out_state, i32, one, dev), max_len, rows,
+          _p(q) if o_ptr else None, ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, _plain(w, "g", g, torch.float32, (rows, H), dev), o_ptr or None,
+          _plain(w, "states", states, torch.float32, (n_states, H, d, d), dev), n_states, H, d, d, code, ws, ws_bytes,
+          _status(w, dev_status, dev))
 
 
-def _cache(where, k_cache, v_cache, k_exp, v_exp):
-    """(n_pages, Hkv, page, type) of a cache, checked."""
-    if k_cache.dim() != 4:
-        _bad(where, f"k_cache: {tuple(k_cache.shape)}")
-    n_pages, hkv, page, d = k_cache.shape
-    kind = {torch.bfloat16: HARTS_BF16, torch.float8_e4m3fn: HARTS_E4M3}.get(k_cache.dtype)
-    if kind is None:
-        _bad(where, f"no cache of {k_cache.dtype}", HARTS_EUNSUPPORTED)
-    _plain(where, "k_cache", k_cache, k_cache.dtype, k_cache.shape)
-    _plain(where, "v_cache", v_cache, k_cache.dtype, k_cache.shape)
-    if d != 128:
-        _bad(where, f"rows of {d}", HARTS_EUNSUPPORTED)
-    for name, e in (("k_exp", k_exp), ("v_exp", v_exp)):
-        if (e is None) != (kind == HARTS_BF16):
-            _bad(where, f"{name} goes with an 8-bit cache")
-        if e is not None:
-            _plain(where, name, e, torch.uint8, (n_pages, hkv, page))
-    return n_pages, hkv, page, kind
+_CACHE_TYPES = {torch.bfloat16: HARTS_BF16, torch.float8_e4m3fn: HARTS_E4M3}
+
+
+def _cache(where, k_cache, v_cache, k_exp, v_exp, dev):
+    """Shape, type and pointers of a cache, checked."""
+    shape = k_cache.shape
+    kind = _CACHE_TYPES.get(k_cache.dtype)
+    if kind is None or len(shape) != 4 or shape[3] != 128:
+        _bad(where, f"no cache of {k_cache.dtype} {tuple(shape)}", HARTS_EUNSUPPORTED)
+    k, v, ke, ve = _plain(where, "k_cache", k_cache, k_cache.dtype, shape, dev), _plain(where, "v_cache", v_cache, k_cache.dtype, shape, dev), None, None
+    if (k_exp is None) != (kind == HARTS_BF16) or (v_exp is None) != (kind == HARTS_BF16):
+        _bad(where, "k_exp and v_exp go with an 8-bit cache, and only with one")
+    if k_exp is not None:
+        ke, ve = _plain(where, "k_exp", k_exp, torch.uint8, shape[:3], dev), _plain(where, "v_exp", v_exp, torch.uint8, shape[:3], dev)
+    return shape, kind, (k, v, ke, ve)
 
 
 def harts_gen_cache_write(k, v, slot, k_cache, v_cache, k_exp=None, v_exp=None, dev_status=None, stream=None):
     """Rows of k, v into slots of a paged cache (harts_gen.h); torch.float8_e4m3fn caches have k_exp, v_exp."""
     w = "harts_gen_cache_write"
-    dev = _one_device(w, k=k, v=v, slot=slot, k_cache=k_cache, v_cache=v_cache, k_exp=k_exp, v_exp=v_exp, dev_status=dev_status)
-    n_pages, hkv, page, kind = _cache(w, k_cache, v_cache, k_exp, v_exp)
+    dev = _device(w, "k_cache", k_cache)
+    (n_pages, hkv, page, _), kind, ptrs = _cache(w, k_cache, v_cache, k_exp, v_exp, dev)
     n = k.shape[0] if k.dim() else 0
-    _plain(w, "slot", slot, torch.int32, (n,))
-    ld_k, ld_v = _rows(w, "k", k, hkv, 128, torch.bfloat16), _rows(w, "v", v, hkv, 128, torch.bfloat16, n)
-    guard, st = _on(dev, stream)
-    with guard:
-        _check(lib.harts_gen_cache_write(n, _p(slot), _p(k), ld_k, _p(v), ld_v, _p(k_cache), _p(v_cache), _p(k_exp), _p(v_exp), n_pages, page, hkv,
-                                         128, kind, _p(dev_status), st), w)
+    shape = (n, hkv, 128)
+    slots = _plain(w, "slot", slot, torch.int32, (n,), dev)
+    ld_k, ld_v = _rows(w, "k", k, shape, torch.bfloat16, dev), _rows(w, "v", v, shape, torch.bfloat16, dev)
+    _call(w, lib.harts_gen_cache_write, dev, stream, n, slots, k.data_ptr(), ld_k, v.data_ptr(), ld_v, *ptrs, n_pages, page, hkv, 128, kind,
+          _status(w, dev_status, dev))
 
 
 def harts_gen_cache_read(k_cache, v_cache, slot, k, v, k_exp=None, v_exp=None, dev_status=None, stream=None):
     """Rows of a paged cache into k, v (bf16, contiguous; either may be None)."""
     w = "harts_gen_cache_read"
-    dev = _one_device(w, slot=slot, k_cache=k_cache, v_cache=v_cache, k=k, v=v, k_exp=k_exp, v_exp=v_exp, dev_status=dev_status)
-    n_pages, hkv, page, kind = _cache(w, k_cache, v_cache, k_exp, v_exp)
+    dev = _device(w, "k_cache", k_cache)
+    (n_pages, hkv, page, _), kind, ptrs = _cache(w, k_cache, v_cache, k_exp, v_exp, dev)
     n = slot.shape[0] if slot.dim() else -1
-    _plain(w, "slot", slot, torch.int32, (n,))
-    for name, t in (("k", k), ("v", v)):
-        if t is not None:
-            _plain(w, name, t, torch.bfloat16, (n, hkv, 128))
-    guard, st = _on(dev, stream)
-    with guard:
-        _check(lib.harts_gen_cache_read(n, _p(slot), _p(k_cache), _p(v_cache), _p(k_exp), _p(v_exp), _p(k), _p(v), n_pages, page, hkv, 128, kind,
-                                        _p(dev_status), st), w)
+    slots = _plain(w, "slot", slot, torch.int32, (n,), dev)
+    out = [None if t is None else _plain(w, name, t, torch.bfloat16, (n, hkv, 128), dev) for name, t in (("k", k), ("v", v))]
+    _call(w, lib.harts_gen_cache_read, dev, stream, n, slots, *ptrs, *out, n_pages, page, hkv, 128, kind, _status(w, dev_status, dev))
 
 
 class GenAttnIndex:
@@ -169,9 +182,10 @@ class GenAttnIndex:
 
     def __init__(self, blob):
         self.host = blob
+        self.host_ptr = blob.ctypes.data_as(_I32P)
         self.n_q, self.Hq, self.Hkv, self.page, self.n_narrow, self.n_wide, self.n_parts = map(int, blob[:7])
         n = _sz(0)
-        _check(lib.harts_gen_attn_workspace_bytes(blob.ctypes.data_as(_I32P), C.byref(n)), "harts_gen_attn_workspace_bytes")
+        _check(lib.harts_gen_attn_workspace_bytes(self.host_ptr, C.byref(n)), "harts_gen_attn_workspace_bytes")
         self.workspace_bytes = n.value
         self.dev = None
 
@@ -211,19 +225,13 @@ def harts_gen_attn(index: GenAttnIndex, q, k_cache, v_cache, q_pos, o, lse, scal
     w = "harts_gen_attn"
     if index.dev is None:
         _bad(w, "the index has not been uploaded")
-    dev = _one_device(w, q=q, index=index.dev, k_cache=k_cache, v_cache=v_cache, k_exp=k_exp, v_exp=v_exp, q_pos=q_pos, o=o, lse=lse,
-                      workspace=workspace, dev_status=dev_status)
-    n_pages, hkv, page, kind = _cache(w, k_cache, v_cache, k_exp, v_exp)
+    dev = _device(w, "k_cache", k_cache)
+    (n_pages, hkv, page, _), kind, ptrs = _cache(w, k_cache, v_cache, k_exp, v_exp, dev)
     if hkv != index.Hkv or page != index.page:
         _bad(w, f"a cache of {hkv} heads and pages of {page} with an index for {index.Hkv} and {index.page}")
-    ld_q = _rows(w, "q", q, index.Hq, 128, torch.bfloat16, index.n_q)
-    _plain(w, "q_pos", q_pos, torch.int32, (index.n_q,))
-    _plain(w, "o", o, torch.bfloat16, (index.n_q, index.Hq, 128))
-    _plain(w, "lse", lse, torch.float32, (index.n_q, index.Hq))
-    if workspace is not None and not workspace.is_contiguous():
-        _bad(w, "workspace is not contiguous")
-    guard, st = _on(dev, stream)
-    with guard:
-        _check(lib.harts_gen_attn(index.host.ctypes.data_as(_I32P), _p(index.dev), _p(q), ld_q, _p(k_cache), _p(v_cache), _p(k_exp), _p(v_exp),
-                                  n_pages, kind, _p(q_pos), _p(o), _p(lse), scale, _p(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _p(dev_status), st), w)
+    shape = (index.n_q, index.Hq, 128)
+    ws, ws_bytes = _bytes(w, "workspace", workspace, dev)
+    _call(w, lib.harts_gen_attn, dev, stream, index.host_ptr, _plain(w, "index", index.dev, torch.int32, index.host.shape, dev), q.data_ptr(),
+          _rows(w, "q", q, shape, torch.bfloat16, dev), *ptrs, n_pages, kind, _plain(w, "q_pos", q_pos, torch.int32, shape[:1], dev),
+          _plain(w, "o", o, torch.bfloat16, shape, dev), _plain(w, "lse", lse, torch.float32, shape[:2], dev), scale, ws, ws_bytes,
+          _status(w, dev_status, dev))

@@ -14,6 +14,8 @@ def arrays(ix):
     at = b[10:16]
     units = [b[at[i]:at[i] + 8 * b[4 + i]].reshape(-1, 8) for i in range(2)]
     entries = b[at[2]:at[3]].reshape(-1, 4)
+    lists = b[b[18]:b[18] + b[17] + 1] if b[17] else np.zeros(1, np.int32)
+    assert lists[0] == 0 and lists[-1] == len(units[0]) and (np.diff(lists) > 0).all()          # every narrow unit is in one list
     return units, entries, b[at[3]:], b[at[4]:at[4] + ix.n_q + 1], b[at[5]:]
 
 
