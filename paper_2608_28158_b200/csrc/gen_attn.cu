@@ -40,7 +40,7 @@ struct Shape {
     static_assert(CTAS * (bytes + 1024) <= 228 * 1024, "shared memory");
 };
 struct Misc {
-    uint64_t full[5], empty[5];
+    uint64_t kfull[5], kempty[5], vfull[5], vempty[5];
     int dead, stop;      // latch: a wait ran out; what the four warps have seen of it at a unit's end, all the same
 };
 
@@ -84,22 +84,17 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
     const int h = blockIdx.x % t.Hkv, first = t.list_ptr[blockIdx.x / t.Hkv], last = t.list_ptr[blockIdx.x / t.Hkv + 1];
     if (tid == 0) {
         for (int i = 0; i < S::STAGES; i++) {
-            mbar_init(&m.full[i], 1);
-            mbar_init(&m.empty[i], CW);
+            mbar_init(&m.kfull[i], 1);
+            mbar_init(&m.kempty[i], CW);
+            mbar_init(&m.vfull[i], 1);
+            mbar_init(&m.vempty[i], CW);
         }
         m.dead = 0;
         fence_barrier_init();
     }
     __syncthreads();
     const int g = lane >> 2, c = lane & 3;
-    int st = 0;                                   // the ring of stages runs on over the units
-    uint32_t ph = 0;
-    auto next_stage = [&]() {
-        if (++st == S::STAGES) {
-            st = 0;
-            ph ^= 1;
-        }
-    };
+    Ring<S::STAGES> rk, rv;                       // the rings of stages run on over the units
     bool alive = true;
 #pragma unroll 1
     for (int item = first; item < last && alive; item++) {
@@ -119,26 +114,35 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
     if (warp == CW) {
         // ---- pages: a box is up to 64 tokens of one page ----------------------------------------------------------------------------
         const int box = 1 << walk.box_shift, per_tile = TILE >> walk.box_shift;
-        for (int n = 0; n < n_tiles; n++, next_stage()) {
-            if (!(alive = mbar_wait_warp(&m.empty[st], ph ^ 1, status, &m.dead))) break;
+        for (int n = 0; n < n_tiles; n++) {
             const int j0 = tile0 + n * TILE, boxes = (min(k1 - j0, TILE) + box - 1) >> walk.box_shift;
-            unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV, *se = smem + S::exps + st * 2 * S::EXP;
-            if (lane == 0) mbar_expect_tx(&m.full[st], boxes * box * (F8 ? 2 * D + 2 : 4 * D));
-            for (int b = 0; b < boxes; b++) {
-                const int at = (j0 + (b << walk.box_shift)) & (t.page - 1), block = walk.of(n * per_tile + b) * t.Hkv + h;
-                if (lane != 0) continue;
-                if constexpr (F8) {
-                    tma_load_3d(sk + b * box * D, &map_k, 0, at, block, &m.full[st]);
-                    tma_load_3d(sv + b * box * D, &map_v, 0, at, block, &m.full[st]);
-                    bulk_load(se + b * box, k_exp + (int64_t)block * t.page + at, box, &m.full[st]);
-                    bulk_load(se + TILE + b * box, v_exp + (int64_t)block * t.page + at, box, &m.full[st]);
-                } else {
-                    for (int p = 0; p < 2; p++) {
-                        tma_load_3d(sk + p * (S::KV / 2) + b * box * 128, &map_k, p * 64, at, block, &m.full[st]);
-                        tma_load_3d(sv + p * (S::KV / 2) + b * box * 128, &map_v, p * 64, at, block, &m.full[st]);
+            int block[4];
+#pragma unroll
+            for (int b = 0; b < 4; b++) block[b] = b < boxes ? walk.of(n * per_tile + b) * t.Hkv + h : 0;
+#pragma unroll
+            for (int is_v = 0; is_v < 2; is_v++) {
+                Ring<S::STAGES>& r = is_v ? rv : rk;
+                if (!(alive = mbar_wait_warp(is_v ? &m.vempty[r.st] : &m.kempty[r.st], r.ph ^ 1, status, &m.dead))) break;
+                uint64_t* bar = is_v ? &m.vfull[r.st] : &m.kfull[r.st];
+                unsigned char *tile = smem + (2 * r.st + is_v) * S::KV, *se = smem + S::exps + (2 * r.st + is_v) * S::EXP;
+                if (lane == 0) {
+                    mbar_expect_tx(bar, boxes * box * (F8 ? D + 1 : 2 * D));
+#pragma unroll
+                    for (int b = 0; b < 4; b++) {
+                        if (b >= boxes) break;
+                        const int at = (j0 + (b << walk.box_shift)) & (t.page - 1);
+                        const CUtensorMap* map = is_v ? &map_v : &map_k;
+                        if constexpr (F8) {
+                            tma_load_3d(tile + b * box * D, map, 0, at, block[b], bar);
+                            bulk_load(se + b * box, (is_v ? v_exp : k_exp) + (int64_t)block[b] * t.page + at, box, bar);
+                        } else {
+                            for (int p = 0; p < 2; p++) tma_load_3d(tile + p * (S::KV / 2) + b * box * 128, map, p * 64, at, block[b], bar);
+                        }
                     }
                 }
+                r.next();
             }
+            if (!alive) break;
             __syncwarp();
         }
     } else {
@@ -191,16 +195,20 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             top[r][0] = top[r][1] = top2[r][0] = top2[r][1] = -INFINITY;
             sum[r][0] = sum[r][1] = 0.f;
         }
-        for (int n = 0; n < n_tiles; n++, next_stage()) {
-            const int j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
-            if (!(alive = mbar_wait_warp(&m.full[st], ph, status, &m.dead))) break;
-            unsigned char *sk = smem + st * 2 * S::KV, *sv = sk + S::KV;
-            const unsigned char* se = smem + S::exps + st * 2 * S::EXP + 16 * warp;
-            // scores of tokens g and g + 8
-            float s[NR][4];
+        // scores of a tile's tokens 16 warp + g and + 8, in log2 units
+        auto scores = [&](float (&s)[NR][4]) {
+            if (!(alive = mbar_wait_warp(&m.kfull[rk.st], rk.ph, status, &m.dead))) return;
+            const unsigned char* sk = smem + 2 * rk.st * S::KV;
+            float s2[NR][4];                      // two chains of products
 #pragma unroll
-            for (int r = 0; r < NR; r++) s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+            for (int r = 0; r < NR; r++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) s[r][x] = s2[r][x] = 0.f;
+            float kp[2] = {1.f, 1.f};
             if constexpr (F8) {
+                const unsigned char* se = smem + S::exps + 2 * rk.st * S::EXP + 16 * warp;
+                kp[0] = gen_power(se[g]);
+                kp[1] = gen_power(se[g + 8]);
 #pragma unroll
                 for (int x = 0; x < 2; x++) {
                     const unsigned char* src = sk + sw128_chunk(16 * warp + g, 2 * c + x);
@@ -210,7 +218,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     for (int i = 0; i < 4; i++) {
                         const uint32_t a[4] = {widen(w[i]), widen(w8[i]), widen_upper(w[i]), widen_upper(w8[i])};
 #pragma unroll
-                        for (int r = 0; r < NR; r++) mma16816<true>(s[r], a, qb[r][4 * x + i][0], qb[r][4 * x + i][1]);
+                        for (int r = 0; r < NR; r++) mma16816<true>(x ? s2[r] : s[r], a, qb[r][4 * x + i][0], qb[r][4 * x + i][1]);
                     }
                 }
             } else {
@@ -220,74 +228,88 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     uint32_t a[4];
                     ldmatrix_x4(smem_u32(sk) + (ch >> 3) * (S::KV / 2) + sw128_chunk(16 * warp + (lane & 15), ch & 7), a);
 #pragma unroll
-                    for (int r = 0; r < NR; r++) mma16816<false>(s[r], a, qb[r][ks][0], qb[r][ks][1]);
+                    for (int r = 0; r < NR; r++) mma16816<false>(ks & 1 ? s2[r] : s[r], a, qb[r][ks][0], qb[r][ks][1]);
                 }
             }
-            // in log2 units; hidden tokens -inf
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&m.kempty[rk.st]);
+            rk.next();
+#pragma unroll
+            for (int r = 0; r < NR; r++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) s[r][x] = (s[r][x] + s2[r][x]) * (F8 ? f[r][x & 1] * kp[x >> 1] : f[r][x & 1]);
+        };
+        float s[NR][4], ahead[NR][4];
+        if (n_tiles > 0) scores(ahead);
+        for (int n = 0; n < n_tiles && alive; n++) {
+            const int j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
+#pragma unroll
+            for (int r = 0; r < NR; r++)
+#pragma unroll
+                for (int x = 0; x < 4; x++) s[r][x] = ahead[r][x];
+            if (n + 1 < n_tiles) {                // the next tile's products run under this one's softmax
+                scores(ahead);
+                if (!alive) break;
+            }
+            if (!(alive = mbar_wait_warp(&m.vfull[rv.st], rv.ph, status, &m.dead))) break;
+            unsigned char* sv = smem + (2 * rv.st + 1) * S::KV;
             const bool edge = j0 < u.k0 || j0 + TILE > min(near, u.k1);
-            float kp[2] = {1.f, 1.f}, ve[2] = {0.f, 0.f};
+            float ve[2] = {0.f, 0.f};
             if constexpr (F8)
 #pragma unroll
                 for (int y = 0; y < 2; y++) {
-                    kp[y] = gen_power(se[g + 8 * y]);
-                    const int e = se[TILE + g + 8 * y];
+                    const int e = smem[S::exps + (2 * rv.st + 1) * S::EXP + 16 * warp + g + 8 * y];
                     ve[y] = e == 255 ? __uint_as_float(0x7fffffffu) : (float)(e - 127);
                 }
-            uint32_t pb[NR][2];
-            bool any_raise = false;
-            float raise_by[NR][2];
+            if (edge)                             // hidden tokens: -inf
 #pragma unroll
-            for (int r = 0; r < NR; r++) {
-                float mx[2], mx2[2];
-#pragma unroll
-                for (int x = 0; x < 4; x++) s[r][x] *= F8 ? f[r][x & 1] * kp[x >> 1] : f[r][x & 1];
-                if (edge)
+                for (int r = 0; r < NR; r++)
 #pragma unroll
                     for (int x = 0; x < 4; x++) {
                         const int key = key0 + g + 8 * (x >> 1);
                         if (key < u.k0 || key >= min(limit[r][x & 1], k1)) s[r][x] = -INFINITY;
                     }
+            // maxima are looked for only where some score is 2^8 above what its row goes by (or has nothing to go by yet)
+            bool over = false;
 #pragma unroll
-                for (int y = 0; y < 2; y++) {
-                    mx[y] = fmaxf(s[r][y], s[r][2 + y]);
-                    if constexpr (F8) mx2[y] = fmaxf(s[r][y] + ve[0], s[r][2 + y] + ve[1]);
+            for (int r = 0; r < NR; r++)
 #pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) {
-                        mx[y] = fmaxf(mx[y], __shfl_xor_sync(~0u, mx[y], x));
-                        if constexpr (F8) mx2[y] = fmaxf(mx2[y], __shfl_xor_sync(~0u, mx2[y], x));
-                    }
-                    if (mx[y] > top[r][y] + RAISE || (top[r][y] == -INFINITY && mx[y] > -INFINITY)) {
-                        const float by = ex2(top[r][y] - mx[y]);          // from -inf: 0, and all sums are 0
-                        sum[r][y] *= by;
-                        top[r][y] = mx[y];
-                        if constexpr (!F8) {
-                            raise_by[r][y] = by;
-                            any_raise = true;
-                        }
-                    } else if constexpr (!F8) {
-                        raise_by[r][y] = 1.f;
-                    }
-                    if constexpr (F8) {
-                        raise_by[r][y] = 1.f;
-                        if (mx2[y] > top2[r][y] + RAISE || (top2[r][y] == -INFINITY && mx2[y] > -INFINITY)) {
-                            raise_by[r][y] = ex2(top2[r][y] - mx2[y]);
-                            top2[r][y] = mx2[y];
-                            any_raise = true;
-                        }
-                    }
+                for (int x = 0; x < 4; x++) {
+                    over |= s[r][x] > top[r][x & 1] + RAISE;
+                    if constexpr (F8) over |= s[r][x] + ve[x >> 1] > top2[r][x & 1] + RAISE;
                 }
-            }
-            if (__any_sync(~0u, any_raise)) {
+            if (__any_sync(~0u, over)) {
 #pragma unroll
                 for (int r = 0; r < NR; r++)
 #pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        acc[r][j][0] *= raise_by[r][0];
-                        acc[r][j][1] *= raise_by[r][1];
-                        acc[r][j][2] *= raise_by[r][0];
-                        acc[r][j][3] *= raise_by[r][1];
+                    for (int y = 0; y < 2; y++) {
+                        float mx = fmaxf(s[r][y], s[r][2 + y]), mx2 = F8 ? fmaxf(s[r][y] + ve[0], s[r][2 + y] + ve[1]) : 0.f;
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) {
+                            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
+                            if constexpr (F8) mx2 = fmaxf(mx2, __shfl_xor_sync(~0u, mx2, x));
+                        }
+                        float by = 1.f;           // (from -inf: 0, and all sums are 0)
+                        if (mx > top[r][y] + RAISE) {
+                            by = ex2(top[r][y] - mx);
+                            sum[r][y] *= by;
+                            top[r][y] = mx;
+                        }
+                        if constexpr (F8) {
+                            by = 1.f;
+                            if (mx2 > top2[r][y] + RAISE) {
+                                by = ex2(top2[r][y] - mx2);
+                                top2[r][y] = mx2;
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 8; j++) {
+                            acc[r][j][y] *= by;
+                            acc[r][j][2 + y] *= by;
+                        }
                     }
             }
+            uint32_t pb[NR][2];
 #pragma unroll
             for (int r = 0; r < NR; r++) {
                 float p[4];
@@ -369,7 +391,8 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&m.empty[st]);
+            if (lane == 0) mbar_arrive(&m.vempty[rv.st]);
+            rv.next();
         }
         // ---- the four warps' parts joined -----------------------------------------------------------------------------------------
         float* so = reinterpret_cast<float*>(smem + S::joint);

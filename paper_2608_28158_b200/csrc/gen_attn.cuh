@@ -60,6 +60,19 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Position in a ring of N stages, and the parity of its barriers in this lap.
+template <int N>
+struct Ring {
+    int st = 0;
+    uint32_t ph = 0;
+    __device__ __forceinline__ void next() {
+        if (++st == N) {
+            st = 0;
+            ph ^= 1;
+        }
+    }
+};
+
 // The pages of a unit's boxes (up to 64 tokens of one page), asked for 32 at a time by a whole warp and a batch ahead of their use: a load for
 // each box, by the thread that has to wait for it, is what the kernels' time went into (3 x 90,000 tokens x 8 heads 116 -> XX us).
 struct PageWalk {
