@@ -196,7 +196,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             sum[r][0] = sum[r][1] = 0.f;
         }
         // scores of a tile's tokens 16 warp + g and + 8, in log2 units
-        auto scores = [&](float (&s)[NR][4]) {
+        auto scores = [&](auto& s) {
             if (!(alive = mbar_wait_warp(&m.kfull[rk.st], rk.ph, status, &m.dead))) return;
             const unsigned char* sk = smem + 2 * rk.st * S::KV;
             float s2[NR][4];                      // two chains of products
@@ -239,18 +239,20 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
 #pragma unroll
                 for (int x = 0; x < 4; x++) s[r][x] = (s[r][x] + s2[r][x]) * (F8 ? f[r][x & 1] * kp[x >> 1] : f[r][x & 1]);
         };
-        float s[NR][4], ahead[NR][4];
-        if (n_tiles > 0) scores(ahead);
+        constexpr bool EARLY = NR == 1;           // (the registers of 16 rows do not allow it)
+        float s[NR][4], ahead[EARLY ? NR : 1][4];
+        if constexpr (EARLY)
+            if (n_tiles > 0) scores(ahead);
         for (int n = 0; n < n_tiles && alive; n++) {
             const int j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
+            if constexpr (EARLY) {                // the next tile's products run under this one's softmax
 #pragma unroll
-            for (int r = 0; r < NR; r++)
-#pragma unroll
-                for (int x = 0; x < 4; x++) s[r][x] = ahead[r][x];
-            if (n + 1 < n_tiles) {                // the next tile's products run under this one's softmax
-                scores(ahead);
-                if (!alive) break;
+                for (int x = 0; x < 4; x++) s[0][x] = ahead[0][x];
+                if (n + 1 < n_tiles) scores(ahead);
+            } else {
+                scores(s);
             }
+            if (!alive) break;
             if (!(alive = mbar_wait_warp(&m.vfull[rv.st], rv.ph, status, &m.dead))) break;
             unsigned char* sv = smem + (2 * rv.st + 1) * S::KV;
             const bool edge = j0 < u.k0 || j0 + TILE > min(near, u.k1);

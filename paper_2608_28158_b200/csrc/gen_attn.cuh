@@ -73,8 +73,8 @@ struct Ring {
     }
 };
 
-// The pages of a unit's boxes (up to 64 tokens of one page), asked for 32 at a time by a whole warp and a batch ahead of their use: a load for
-// each box, by the thread that has to wait for it, is what the kernels' time went into (3 x 90,000 tokens x 8 heads 116 -> XX us).
+// The pages of a unit's boxes (up to 64 tokens of one page), asked for 32 at a time by a whole warp and a batch ahead of their use, so that
+// copies do not wait for table entries.
 struct PageWalk {
     const int32_t* pages;
     int tile0, end, box_shift, page_shift, lane, batch = -1, now = 0, next = 0;

@@ -18,9 +18,7 @@ using namespace harts::gen_attn;
 constexpr int TILE = 64;
 constexpr int MIXED = 2 * TILE;         // limits this near to each other share a run
 constexpr int LEAST = 256;              // tokens a wide unit is not cut below
-// CTAs wanted, all key heads together: as many as the GPU holds.  Of the wide kernel three quarters of that: what is left lets the narrow one
-// start beside it (64 branches of a prompt of 16,421 tokens 84 -> 78 us).
-constexpr int SMS = 148, WIDE_CTAS = SMS * 3 / 2;
+constexpr int SMS = 148;
 constexpr int PIECE = 2;                // tiles that a unit costs besides its own, and that are not cut off one
 // Below so many tokens (one short unit an SM, all key heads) a call's time is the kernels' latency, and the narrow kernel's is the shorter:
 // 28 rows x 700 tokens 12.4 against 16.4 us.  Above, from 16 rows on the wide one (agentic trees, 32 rows x 900: 92 against 119 us).
@@ -35,7 +33,7 @@ struct Index {
     std::vector<Unit> narrow, wide;
     std::vector<Entry> entries;
     std::vector<int32_t> part_ptr, part, list_ptr;
-    int32_t n_parts = 0, merged = 0, max_page = -1;
+    int32_t n_parts = 0, merged = 0, max_page = -1, beside = 0;
 };
 
 bool forest_ok(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const int32_t* off, const int32_t* len) {
@@ -136,6 +134,32 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
             add(v, own_from, (int)most, false, e);
         }
     }
+    // Rows of a narrow unit: eight where no run of few rows has more (the kernel is the faster of the two).
+    auto tiles_of = [](int a, int b) { return (int64_t)(b + TILE - 1) / TILE - a / TILE; };
+    int block_rows = 8;
+    for (const Range& r : ranges)
+        if (!r.wide && (int64_t)r.n_entries * G > 8) block_rows = NARROW_ROWS;
+    if (G > 8) block_rows = NARROW_ROWS;
+    // A little wide work beside much narrow work costs more as a kernel of its own than as blocks of few rows that read its tokens again
+    // (64 branches of 1,300 tokens on a prompt of 64: 52 -> 43 us).
+    auto blocks = [&](const Range& r, int rows) { return ((int64_t)r.n_entries * G + rows - 1) / rows; };
+    int64_t narrow_tiles = 0, wide_tiles = 0, again = 0;
+    for (const Range& r : ranges)
+        if (r.wide) {
+            wide_tiles += blocks(r, WIDE_ROWS) * tiles_of(r.a, r.b);
+            again += blocks(r, block_rows) * tiles_of(r.a, r.b);
+        } else {
+            narrow_tiles += blocks(r, block_rows) * tiles_of(r.a, r.b);
+        }
+    if (8 * again <= narrow_tiles) {
+        for (Range& r : ranges) r.wide = false;
+        wide_tiles = 0;
+    }
+    // Much of both: one CTA of either kernel on an SM, products of the one under the memory traffic of the other (64 branches on a prompt of
+    // 16,421 tokens, 28 wide and 38 narrow tiles an SM: 80 -> 61 us).  A tile takes such a CTA 1.5 times what it takes the kernel alone, so
+    // beyond 2 : 1 they run one after the other, each with the GPU to itself.
+    const bool beside = wide_tiles > 0 && narrow_tiles <= 2 * wide_tiles && wide_tiles <= 2 * narrow_tiles;
+    ix.beside = beside;
     std::stable_sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.b - x.a > y.b - y.a; });
     std::vector<std::vector<int32_t>> parts(n_q);
     int64_t n_parts = 0;
@@ -149,22 +173,23 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
         return n_parts <= INT32_MAX - (1 << 20);
     };
 
-    // The wide kernel's runs: the shortest pieces that still make one wave; with more units than that anyway, pieces of half a CTA's share.
+    // The wide kernel's runs: the shortest pieces that still make one wave; with more units than that anyway, pieces of two thirds of a CTA's
+    // share.
     int64_t total = 0, units = 0, lo = LEAST, hi = LEAST;
-    auto blocks = [&](const Range& r) { return ((int64_t)r.n_entries * G + WIDE_ROWS - 1) / WIDE_ROWS; };
     for (const Range& r : ranges)
         if (r.wide) {
-            total += blocks(r) * (r.b - r.a) * Hkv;
-            units += blocks(r) * Hkv;
+            total += blocks(r, WIDE_ROWS) * (r.b - r.a) * Hkv;
+            units += blocks(r, WIDE_ROWS) * Hkv;
             hi = std::max<int64_t>(hi, r.b - r.a);
         }
-    if (units > WIDE_CTAS) lo = hi = std::max<int64_t>(LEAST, total / (2 * WIDE_CTAS));
+    const int64_t want = SMS * (beside ? 1 : 2);
+    if (units > want) lo = hi = std::max<int64_t>(LEAST, 2 * total / (3 * want));
     while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
         int64_t n = 0;
         for (const Range& r : ranges)
-            if (r.wide) n += blocks(r) * Hkv * ((r.b - r.a + mid - 1) / mid);
-        if (n <= WIDE_CTAS) hi = mid;
+            if (r.wide) n += blocks(r, WIDE_ROWS) * Hkv * ((r.b - r.a + mid - 1) / mid);
+        if (n <= want) hi = mid;
         else lo = mid + 1;
     }
     for (const Range& r : ranges) {
@@ -177,22 +202,19 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
     }
     std::stable_sort(ix.wide.begin(), ix.wide.end(), [](const Unit& x, const Unit& y) { return x.k1 - x.k0 > y.k1 - y.k0; });
 
-    // The narrow kernel's: queries in blocks of 16 rows (a query of more heads is several blocks that are cut alike), and a list for every CTA
+    // The narrow kernel's: queries in blocks of 8 or 16 rows (a query of more heads is several blocks that are cut alike), and a list for every CTA
     // until its share of the tiles is full; a run that crosses a list's end is cut there.
-    const int per_block = std::max(1, NARROW_ROWS / G);
+    const int per_block = std::max(1, block_rows / G);
     int64_t tiles = 0, strips = 0;
-    int most = 0;                                  // rows of a unit
     const int chunks = (G + NARROW_ROWS - 1) / NARROW_ROWS;
-    auto tiles_of = [](int a, int b) { return (int64_t)(b + TILE - 1) / TILE - a / TILE; };
     for (const Range& r : ranges)
         if (!r.wide) {
             const int64_t n = (r.n_entries + per_block - 1) / per_block * (int64_t)chunks;
             strips += n;
             tiles += n * tiles_of(r.a, r.b);
-            most = std::max(most, std::min(r.n_entries * G, std::min(per_block * G, NARROW_ROWS)));
         }
     if (strips) {
-        const int64_t ctas = SMS * (most <= 8 ? 3 : 2), lists = std::max<int64_t>(1, ctas / Hkv);
+        const int64_t ctas = SMS * (beside ? 1 : block_rows == 8 ? 3 : 2), lists = std::max<int64_t>(1, ctas / Hkv);
         // the lists for a share of tiles: piece(range, first query, queries, from, to) and closed() in order; how many there are
         auto fill = [&](int64_t share, auto piece, auto closed) {
             int64_t full = 0, n_lists = 0;        // full: tiles of the list that is being filled
@@ -298,6 +320,7 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
         blob[WORDS] = (int32_t)total;
         for (const Unit& u : ix.narrow) blob[NARROW_MAX] = std::max(blob[NARROW_MAX], u.n);
         for (int i = 0; i < 6; i++) blob[NARROW + i] = (int32_t)at[i];
+        blob[BESIDE] = ix.beside;
         blob[N_LISTS] = std::max<int32_t>(0, (int32_t)ix.list_ptr.size() - 1);
         blob[LIST_PTR] = (int32_t)at[6];
         auto put = [&](int i, const void* p, int64_t words) {
