@@ -31,6 +31,7 @@ int32_t gen_la_walk(const GenLaArgs& a);          // gen_la_walk.cu: token by to
 // Chunked form (bf16, d = 128): a sequence is one item, or several segments of whole chunks that one item each walks.
 struct GenItems {
     const int32_t* count;     // device: items there are
+    int32_t* ticket;          // device: 0; how many CTAs have drawn
     const int4* items;        // device: first row, rows, start state (>= 0: in the pool, -1: zero, -2 - i: starts[i]), last state's place or -1
     float* starts;            // [item, H, 128, 128] start states of segments
 };

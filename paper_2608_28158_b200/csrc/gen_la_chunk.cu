@@ -51,56 +51,80 @@ Sizes sizes_of(const GenLaArgs& a) {
 }
 
 constexpr int PLAN_THREADS = 512;
-// Items in the order of the sequences, and each sequence's {first item, items, start state, -}.
+// The items: whole segments first, in the order of the sequences, then what is left of each (the walk's CTAs draw them from a counter, so the
+// short ones fill the gaps).  chains: each sequence's {first whole segment, items, start state, item of the rest or -1}.
 __global__ void __launch_bounds__(PLAN_THREADS)
 plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, int* follows, int4* chains) {
-    __shared__ int warp_sum[PLAN_THREADS / 32], base;
+    __shared__ int2 warp_sum[PLAN_THREADS / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) base = 0;
-    __syncthreads();
     const int rows = L ? L * BT : INT32_MAX;
+    auto look_up = [&](int i, GenSeq& s, bool report) {           // {whole segments, rest}
+        if (i >= a.n_seq) return make_int2(0, 0);
+        if (!gen_seq(a, i, s)) {
+            if (report) gen_report(a.dev_status, i);
+            return make_int2(0, 0);
+        }
+        if (s.out < 0 && !(a.o && s.len > 0)) return make_int2(0, 0);
+        return make_int2(s.len / rows, s.len == 0 || s.len % rows != 0);
+    };
+    int whole = 0;
+    GenSeq s;
+    for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) whole += look_up(i0 + tid, s, true).x;
+    for (int d = 16; d > 0; d >>= 1) whole += __shfl_xor_sync(~0u, whole, d);
+    if (lane == 0) warp_sum[warp].x = whole;
+    __syncthreads();
+    whole = 0;
+    for (int w = 0; w < PLAN_THREADS / 32; w++) whole += warp_sum[w].x;
+    __syncthreads();
+    int2 base = make_int2(0, whole);
     for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
-        GenSeq s;
-        int n = 0;
-        if (i < a.n_seq) {
-            if (!gen_seq(a, i, s)) gen_report(a.dev_status, i);
-            else if (s.out >= 0 || (a.o && s.len > 0)) n = s.len == 0 ? 1 : (s.len - 1) / rows + 1;
-        }
-        int upto = n;
+        const int2 n = look_up(i, s, false);
+        int2 upto = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(~0u, upto, d);
-            if (lane >= d) upto += y;
+            const int x = __shfl_up_sync(~0u, upto.x, d), y = __shfl_up_sync(~0u, upto.y, d);
+            if (lane >= d) {
+                upto.x += x;
+                upto.y += y;
+            }
         }
         if (lane == 31) warp_sum[warp] = upto;
         __syncthreads();
-        int ahead = base;
-        for (int w = 0; w < warp; w++) ahead += warp_sum[w];
-        upto += ahead;
-        if (n > 0 && upto > max_items) {               // rows that sequences share: more items than the rows allow
-            gen_report(a.dev_status, i);
-            n = 0;
-        } else if (n > 0) {
-            const int first = upto - n;
-            for (int j = 0; j < n; j++) {
-                items[first + j] = make_int4(s.begin + j * rows, j + 1 < n ? rows : s.len - j * rows, n > 1 ? -2 - (first + j) : s.in, j + 1 < n ? -1 : s.out);
-                follows[first + j] = j + 1 < n;
+        int2 at = make_int2(base.x + upto.x - n.x, base.y + upto.y - n.y);
+        for (int w = 0; w < PLAN_THREADS / 32; w++) {
+            if (w < warp) {
+                at.x += warp_sum[w].x;
+                at.y += warp_sum[w].y;
             }
-            chains[i] = make_int4(first, n, s.in, 0);
+            base.x += warp_sum[w].x;
+            base.y += warp_sum[w].y;
         }
-        if (n == 0 && i < a.n_seq) chains[i] = make_int4(0, 0, -1, 0);
-        __syncthreads();
-        if (tid == PLAN_THREADS - 1) base = min(upto, max_items);
+        const int items_here = n.x + n.y;
+        if (items_here > 0 && (whole > max_items || at.y + n.y > max_items)) {        // rows that sequences share: more items than the rows allow
+            gen_report(a.dev_status, i);
+            chains[i] = make_int4(0, 0, -1, -1);
+        } else if (i < a.n_seq) {
+            for (int j = 0; j < items_here; j++) {
+                const int item = j < n.x ? at.x + j : at.y;
+                const bool last = j + 1 == items_here;
+                items[item] = make_int4(s.begin + j * rows, j < n.x ? rows : s.len - j * rows, items_here > 1 ? -2 - item : s.in, last ? s.out : -1);
+                follows[item] = !last;
+            }
+            chains[i] = make_int4(at.x, items_here, s.in, n.y ? at.y : -1);
+        }
         __syncthreads();
     }
-    if (tid == 0) *count = base;
+    if (tid == 0) {
+        count[0] = whole > max_items ? 0 : min(base.y, max_items);
+        count[1] = 0;                             // the walk's counter
+    }
 }
 
 // ---- sums of segments --------------------------------------------------------------------------------------------------------
 constexpr int PANEL = BT * 128, TILE = 2 * PANEL, STAGE = 2 * TILE, STAGES = 2, SUM_THREADS = 288, SUM_WARPS = 8;
 struct SumMisc {
-    float w[MAX_L * BT];
+    float w[(MAX_L * BT + 255) / 256 * 256];
     float warp_sum[SUM_WARPS];
     uint64_t full[STAGES], ready[STAGES], done[STAGES];
     uint32_t tmem;
@@ -174,10 +198,10 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
             }
         }
     } else {
-        // ---- weights e^{B_end - B_j}: L / 4 tokens in a row per thread, summed from the end --------------------------------------------
-        for (int e = tid; e < len; e += 256) m.w[e] = g[(size_t)(begin + e) * H + h] * LOG2E;
+        // ---- weights e^{B_end - B_j}: some tokens in a row per thread, summed from the end --------------------------------------------
+        const int per = (len + 255) / 256;         // (behind the segment: nothing decays)
+        for (int e = tid; e < per * 256; e += 256) m.w[e] = e < len ? g[(size_t)(begin + e) * H + h] * LOG2E : 0.f;
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        const int per = len / 256;
         float own = 0.f;
         for (int e = 0; e < per; e++) own += m.w[tid * per + e];
         float behind = own;                       // of this thread and the ones behind it in the warp
@@ -268,7 +292,8 @@ scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const 
     const size_t off = (size_t)(blockIdx.x * 256 + threadIdx.x) * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (chain.z >= 0) s = *reinterpret_cast<const float4*>(states + ((size_t)chain.z * H + h) * (D * D) + off);
-    auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)(chain.x + j) * H + h) * (D * D) + off); };
+    auto item = [&](int j) { return j + 1 == chain.y && chain.w >= 0 ? chain.w : chain.x + j; };
+    auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)item(j) * H + h) * (D * D) + off); };
     for (int j0 = 0; j0 < chain.y; j0 += AHEAD) {
         float4 u[AHEAD];
         float e[AHEAD];
@@ -276,7 +301,7 @@ scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const 
         for (int j = 0; j < AHEAD; j++)
             if (j0 + j + 1 < chain.y) {
                 u[j] = *at(j0 + j);
-                e[j] = gamma[(size_t)(chain.x + j0 + j) * H + h];
+                e[j] = gamma[(size_t)item(j0 + j) * H + h];
             }
 #pragma unroll
         for (int j = 0; j < AHEAD; j++)
@@ -309,7 +334,7 @@ int32_t gen_la_chunks(const GenLaArgs& a) {
     float *gamma = reinterpret_cast<float*>(ws + z.gamma), *starts = reinterpret_cast<float*>(ws + z.starts);
     plan_kernel<<<1, PLAN_THREADS, 0, a.stream>>>(a, z.L, (int)z.max_items, count, items, follows, chains);
     if (cudaGetLastError() != cudaSuccess) return HARTS_ECUDA;
-    const GenItems gen{count, items, starts};
+    const GenItems gen{count, count + 1, items, starts};
     if (z.L) {
         CUtensorMap mk, mv;
         int32_t rc;

@@ -255,7 +255,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
             if (GEN ? init_slot != -1 : init_slot >= 0) {
                 const size_t from = (size_t)init_slot * H + h;
                 const float* src = (GEN ? state_of(init_slot, h) : slots + from * (D * D)) + in_state;
-                if (ticket) alive = flag_wait_warp(flags + from * SLICES + slice, 1, status, &m.dead);
+                if (!GEN && ticket) alive = flag_wait_warp(flags + from * SLICES + slice, 1, status, &m.dead);
                 // a thread's row is 512 bytes from the next one's: whole sectors at a time, where the array allows it
                 if ((reinterpret_cast<uintptr_t>(slots) & 31) == 0) {
 #pragma unroll
@@ -880,7 +880,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if (boundary == c) {
                     if (!(alive = wait(&m.exported[re.i], re.ph))) break;
                     re.next();
-                    if (ticket && lane == 0) flag_set(flags + ((size_t)req * H + h) * SLICES + slice);
+                    if (!GEN && ticket && lane == 0) flag_set(flags + ((size_t)req * H + h) * SLICES + slice);
                     req++;
                     boundary = req < req_hi ? tb.slot_chunk[req] : -1;
                 }
@@ -931,7 +931,7 @@ int32_t launch_gen(const GenLaArgs& a, const GenItems& items, int64_t max_items)
     const int64_t n = max_items * a.H * (D / NV);
     return launch_after(pipe_fwd_kernel<NV, true>, n < sm_count() ? (int)n : sm_count(), NT, S::bytes, a.stream, harts_la_tables_t{}, items, 0, 0, a.H,
                         mq, mk, mv, mq, mo, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, (const __nv_bfloat16*)nullptr, a.g,
-                        (__nv_bfloat16*)a.o, a.states, 0, a.dev_status, (const int32_t*)nullptr, (int*)nullptr, (int*)nullptr) == cudaSuccess
+                        (__nv_bfloat16*)a.o, a.states, 0, a.dev_status, (const int32_t*)nullptr, (int*)nullptr, items.ticket) == cudaSuccess
                ? HARTS_OK : HARTS_ECUDA;
 }
 
