@@ -37,7 +37,7 @@ Sizes sizes_of(const GenLaArgs& a) {
     z.L = 0;
     if (longest > 8 && 2 * longest > 3 * share) {
         const int64_t L = room > 0 ? (chunks + room - 1) / room : (share + 1) / 2;
-        z.L = (int)(L < 4 ? 4 : L > MAX_L ? MAX_L : (L + 3) / 4 * 4);
+        z.L = (int)(L < 4 ? 4 : L > MAX_L ? MAX_L : L);
     }
     z.max_items = a.n_seq + (z.L ? chunks / z.L : 0);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(PLAN_THREADS)
 plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, int* follows, int4* chains) {
     __shared__ int2 warp_sum[PLAN_THREADS / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    let_next_launch();
     const int rows = L ? L * BT : INT32_MAX;
     auto look_up = [&](int i, GenSeq& s, bool report) {           // {whole segments, rest}
         if (i >= a.n_seq) return make_int2(0, 0);
@@ -136,6 +137,7 @@ constexpr int SUM_BYTES = STAGES * STAGE + 2 * TILE + sizeof(SumMisc) + 1024;
 __global__ void __launch_bounds__(SUM_THREADS, 2)
 sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const float* __restrict__ g, int H,
            const GenItems gen, const int* __restrict__ follows, float* __restrict__ gamma, int* status) {
+    let_next_launch();
     after_previous();
     const int item = blockIdx.x / H, h = blockIdx.x % H;
     if (item >= *gen.count || !follows[item]) return;
@@ -236,18 +238,10 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
                 const int e = tid + u * 256, t = (e >> 3) & (BT - 1), off = (e >> 9) * PANEL + sw128_chunk(t, e & 7);
                 const float w = m.w[c * BT + t];
                 uint4 y = *reinterpret_cast<const uint4*>(tile + off), z, z2;
-                auto terms = [&](uint32_t& t1, uint32_t& t2, uint32_t& t3) {
-                    float p0 = __uint_as_float(t1 << 16) * w, p1 = __uint_as_float(t1 & 0xffff0000u) * w;
-                    t1 = pack_bf16(p0, p1);
-                    p0 -= __uint_as_float(t1 << 16);
-                    p1 -= __uint_as_float(t1 & 0xffff0000u);
-                    t2 = pack_bf16(p0, p1);
-                    t3 = pack_bf16(p0 - __uint_as_float(t2 << 16), p1 - __uint_as_float(t2 & 0xffff0000u));
-                };
-                terms(y.x, z.x, z2.x);
-                terms(y.y, z.y, z2.y);
-                terms(y.z, z.z, z2.z);
-                terms(y.w, z.w, z2.w);
+                three_terms(y.x, z.x, z2.x, f2(w, w));
+                three_terms(y.y, z.y, z2.y, f2(w, w));
+                three_terms(y.z, z.z, z2.z, f2(w, w));
+                three_terms(y.w, z.w, z2.w, f2(w, w));
                 *reinterpret_cast<uint4*>(tile + off) = y;
                 *reinterpret_cast<uint4*>(rest + off) = z;
                 *reinterpret_cast<uint4*>(rest + TILE + off) = z2;
@@ -282,9 +276,10 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 }
 
 // ---- start states of segments: starts[i] holds U_i on entry and S_i afterwards; four elements a thread -------------------------------
-constexpr int AHEAD = 8;
+constexpr int BATCH = 8;
 __global__ void __launch_bounds__(256)
 scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const int4* __restrict__ chains, const float* __restrict__ gamma, int H) {
+    let_next_launch();
     after_previous();
     const int4 chain = chains[blockIdx.z];
     if (chain.y < 2) return;
@@ -294,17 +289,17 @@ scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const 
     if (chain.z >= 0) s = *reinterpret_cast<const float4*>(states + ((size_t)chain.z * H + h) * (D * D) + off);
     auto item = [&](int j) { return j + 1 == chain.y && chain.w >= 0 ? chain.w : chain.x + j; };
     auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)item(j) * H + h) * (D * D) + off); };
-    for (int j0 = 0; j0 < chain.y; j0 += AHEAD) {
-        float4 u[AHEAD];
-        float e[AHEAD];
+    for (int j0 = 0; j0 < chain.y; j0 += BATCH) {
+        float4 u[BATCH];
+        float e[BATCH];
 #pragma unroll
-        for (int j = 0; j < AHEAD; j++)
+        for (int j = 0; j < BATCH; j++)
             if (j0 + j + 1 < chain.y) {
                 u[j] = *at(j0 + j);
                 e[j] = gamma[(size_t)item(j0 + j) * H + h];
             }
 #pragma unroll
-        for (int j = 0; j < AHEAD; j++)
+        for (int j = 0; j < BATCH; j++)
             if (j0 + j < chain.y) {
                 *at(j0 + j) = s;
                 if (j0 + j + 1 < chain.y) {

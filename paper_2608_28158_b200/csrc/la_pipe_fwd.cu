@@ -152,17 +152,6 @@ __device__ __forceinline__ void mma_steps(uint32_t d, uint32_t a, uint32_t b, ui
     for (int ks = 1; ks < STEPS; ks++) mma_lo<true>(d, a + ks * SA + (ks >> 2) * GA, b + ks * SB + (ks >> 2) * GB, idesc);
 }
 
-// A weighted pair of keys, w k, as three terms of bf16.
-__device__ __forceinline__ void three_terms(uint32_t& x, uint32_t& y, uint32_t& z, F2 w) {
-    float a, b;
-    f2_split(f2_mul(f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)), w), a, b);
-    x = pack_bf16(a, b);
-    a -= __uint_as_float(x << 16);
-    b -= __uint_as_float(x & 0xffff0000u);
-    y = pack_bf16(a, b);
-    z = pack_bf16(a - __uint_as_float(y << 16), b - __uint_as_float(y & 0xffff0000u));
-}
-
 template <int NV, bool GEN>
 __global__ void __launch_bounds__(NT, 1)
 pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int n_items, int H, const __grid_constant__ CUtensorMap map_q,
@@ -189,7 +178,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
         }
         for (int i = 0; i < 2; i++) {
             mbar_init(&m.a_full[i], 1);
-            mbar_init(&m.ready[i], GEN ? NW / 64 : NW / 32);
+            mbar_init(&m.ready[i], NW / 32);
             mbar_init(&m.masked[i], NW / 64);
             mbar_init(&m.u_full[i], 1);
             mbar_init(&m.s_full[i], NS / 32);
@@ -346,11 +335,53 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
 #pragma unroll
             for (int u = 0; u < 8; u++)
                 if (!GEN || u < 4) *reinterpret_cast<uint4*>(smem + S::p + (u >> 2) * PANEL + sw128_chunk(t, 4 + (u & 3))) = make_uint4(0, 0, 0, 0);
+        // GEN: rows from .. to - 1 of a panel of weighted keys, as three terms.  The warps that mask take a quarter of them.
+        bool added = false;                       // there is a sum before this chunk's
+        auto weigh = [&](const Record& rd, int panel, int from, int to) {
+            if (!rd.step) return true;
+            // the tiles of second and third terms: the sum before this one has been made
+            if (added) {
+                if (!wait(&m.u_full[rl.i], rl.ph)) return false;
+                rl.next();
+            }
+            added = true;
+            unsigned char *sk = smem + rg.i * S::STAGE + S::K + panel * PANEL, *sl = smem + S::lo + panel * PANEL;
+#pragma unroll 1
+            for (int t0 = from + (lane >> 3); t0 < to; t0 += 16) {
+                uint4 y[4];
+                float w[4];
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    y[u] = *reinterpret_cast<const uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7));
+                    w[u] = __uint_as_float(rd.w[t0 + 4 * u].x);
+                    if (t0 + 4 * u >= rd.valid) y[u] = make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    uint4 z, z2;
+                    const F2 w2 = f2(w[u], w[u]);
+                    three_terms(y[u].x, z.x, z2.x, w2);
+                    three_terms(y[u].y, z.y, z2.y, w2);
+                    three_terms(y[u].z, z.z, z2.z, w2);
+                    three_terms(y[u].w, z.w, z2.w, w2);
+                    *reinterpret_cast<uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7)) = y[u];
+                    *reinterpret_cast<uint4*>(sl + sw128_chunk(t0 + 4 * u, lane & 7)) = z;
+                    *reinterpret_cast<uint4*>(sl + 2 * PANEL + sw128_chunk(t0 + 4 * u, lane & 7)) = z2;
+                }
+            }
+            return true;
+        };
         for (;;) {
             if (!wait(&m.gates_full[rg.i], rg.ph)) break;
             const Record& rd = m.rows[rg.i];
             if (rd.end) break;
             if (quarter < 2) {                    // P = A .* decay: lanes 0..63 hold the rows
+                if constexpr (GEN) {
+                    if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph) || !weigh(rd, quarter, 48, 64)) break;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&m.ready[ra.i]);
+                }
                 // (behind A of this chunk: the product that read this tile of P two chunks ago, which was issued before it, is done too)
                 if (!wait(&m.a_full[ra.i], ra.ph)) break;
                 tc_fence_after();
@@ -405,38 +436,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph)) break;
                 if constexpr (GEN) {
                     const int valid = rd.valid;
-                    if (rd.step) {
-                        // the tiles of second and third terms: the sum before this one has been made
-                        if (summed) {
-                            if (!wait(&m.u_full[rl.i], rl.ph)) break;
-                            rl.next();
-                        }
-                        summed = true;
-                        unsigned char *sk = smem + rg.i * S::STAGE + S::K + (quarter - 2) * PANEL, *sl = smem + S::lo + (quarter - 2) * PANEL;
-#pragma unroll 1
-                        for (int t0 = lane >> 3; t0 < BT; t0 += 16) {
-                            uint4 y[4];
-                            float w[4];
-#pragma unroll
-                            for (int u = 0; u < 4; u++) {
-                                y[u] = *reinterpret_cast<const uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7));
-                                w[u] = __uint_as_float(rd.w[t0 + 4 * u].x);
-                                if (t0 + 4 * u >= valid) y[u] = make_uint4(0, 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int u = 0; u < 4; u++) {
-                                uint4 z, z2;
-                                const F2 w2 = f2(w[u], w[u]);
-                                three_terms(y[u].x, z.x, z2.x, w2);
-                                three_terms(y[u].y, z.y, z2.y, w2);
-                                three_terms(y[u].z, z.z, z2.z, w2);
-                                three_terms(y[u].w, z.w, z2.w, w2);
-                                *reinterpret_cast<uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7)) = y[u];
-                                *reinterpret_cast<uint4*>(sl + sw128_chunk(t0 + 4 * u, lane & 7)) = z;
-                                *reinterpret_cast<uint4*>(sl + 2 * PANEL + sw128_chunk(t0 + 4 * u, lane & 7)) = z2;
-                            }
-                        }
-                    }
+                    if (!weigh(rd, quarter - 2, 0, 48)) break;
                     if (valid < BT && quarter - 2 < VP) {
                         unsigned char* sv = smem + rg.i * S::STAGE + S::V + (quarter - 2) * PANEL;
 #pragma unroll 1

@@ -385,5 +385,20 @@ __device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
     return r;
 }
 
+// A pair of bf16 values times w as three bf16 terms each, cut off and not rounded: 8 + 8 + 8 bits are all of an fp32 product's.
+__device__ __forceinline__ void three_terms(uint32_t& x, uint32_t& y, uint32_t& z, F2 w) {
+    auto minus_upper = [](float v) { return __uint_as_float((__float_as_uint(v) & 0xffff0000u) ^ 0x80000000u); };
+    F2 r = f2_mul(f2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)), w);
+    float a, b;
+    f2_split(r, a, b);
+    x = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    r = f2_add(r, f2(minus_upper(a), minus_upper(b)));
+    f2_split(r, a, b);
+    y = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    r = f2_add(r, f2(minus_upper(a), minus_upper(b)));
+    f2_split(r, a, b);
+    z = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+
 }  // namespace tc
 }  // namespace harts
