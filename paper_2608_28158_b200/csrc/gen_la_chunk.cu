@@ -314,8 +314,12 @@ scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const 
 
 }  // namespace
 
-// Tokens one by one or chunks: see the figures at the head of gen_la_walk.cu.
-bool gen_la_chunked(const GenLaArgs& a) { return a.dtype == HARTS_BF16 && a.d == 128 && a.max_len > 16; }
+// Tokens one by one or chunks, tokens a sequence: a walk costs about a microsecond a token where states wait for a free SM, a chunk the same
+// for 1 to 64.  200 branches x 32 heads: 12 tokens 292 us, 14 339, a chunk 311; 64 x 16: 61 at 14, 65 at 16, a chunk 64.  Where every state has an SM
+// (8 x 16), 14.6 at 16 and a chunk 18.5.
+bool gen_la_chunked(const GenLaArgs& a) {
+    return a.dtype == HARTS_BF16 && a.d == 128 && a.max_len > ((int64_t)a.n_seq * a.H > 2 * sm_count() ? 12 : 20);
+}
 
 size_t gen_la_chunk_bytes(const GenLaArgs& a) { return sizes_of(a).total; }
 

@@ -139,8 +139,11 @@ int32_t launch(const GenLaArgs& a) {
 }
 template <class T>
 int32_t by_size(const GenLaArgs& a) {
-    const bool few = (int64_t)a.n_seq * a.H <= 2 * sm_count();      // slices of the columns give every SM some of the work
-    if (a.d == 128) return few ? launch<T, 128, 32, 256>(a) : launch<T, 128, 128, 256>(a);
+    // With few states narrow slices of their columns give every SM some of the work; else a thread's 64 values, whose loads are on their way
+    // together, and small CTAs, whose loads and stores overlap with each other's (201 branches x 32 heads of 128: 256 threads and all columns
+    // 149 us, 128 threads and half of them 138, 0.95 of the copy bandwidth)
+    const bool few = (int64_t)a.n_seq * a.H <= sm_count();
+    if (a.d == 128) return few ? launch<T, 128, 32, 256>(a) : launch<T, 128, 64, 128>(a);
     return few ? launch<T, 64, 16, 128>(a) : launch<T, 64, 64, 128>(a);
 }
 

@@ -110,6 +110,7 @@ def test_single_tokens(dtype, d, n, heads):
 def test_short_runs_empty_ones_and_gaps(dtype, d):
     check([0, 1, 2, 3, 7, 8, 9, 16, 5, 0, 11], 3, d, dtype, gaps=2)
     check([3, 0, 8, 1], 130, d, dtype, gaps=1)
+    check([3, 0, 14, 1], 130, d, dtype, gaps=1)
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("fp32", 64), ("fp32", 128)])
@@ -117,7 +118,7 @@ def test_long_runs_token_by_token(dtype, d):
     check([130, 1, 0, 65], 2, d, dtype, gaps=3, strong=True)
 
 
-@pytest.mark.parametrize("lens,heads", [([17], 1), ([63, 64, 65, 1, 0, 128, 129], 2), ([40] * 30, 8), ([190, 1, 777], 16)])
+@pytest.mark.parametrize("lens,heads", [([21], 1), ([63, 64, 65, 1, 0, 128, 129], 2), ([40] * 30, 8), ([190, 1, 777], 16)])
 def test_chunks(lens, heads):
     check(lens, heads, 128, "bf16", gaps=5)
 
@@ -137,7 +138,7 @@ def test_rows_of_a_wider_tensor(dtype, d, lens):
     check(lens, 2, d, dtype, ld=1024, gaps=1)
 
 
-@pytest.mark.parametrize("max_len", [17, 5000])
+@pytest.mark.parametrize("max_len", [17, 21, 5000])
 def test_a_bound_far_above_the_lengths(max_len):
     check([1, 2, 0, 17], 2, 128, "bf16", max_len=max_len)
 
