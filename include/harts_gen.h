@@ -101,7 +101,7 @@ int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache
  * harts_gen_attn_index (host in, host out): work lists for such a forest, one int32 blob; the same blob is copied to the device.
  *   Tokens that several queries see are read once for up to 128 rows (a row: a query and a head of its group), long runs are split over the GPU.
  *   grow: by how many tokens nodes with queries may grow while the index is used: between calls (and replays of a captured call) q_pos may
- *   go up, to node_len - 1 + grow at most, and never below what it was for the index.  node_page has to list the pages of that many tokens.
+ *   go up, to node_len - 1 + grow at most and as far as the node's listed pages go, and never below what it was for the index.
  *   A new branch, a fork, or a query more or less needs a new index.
  *   cap_words: capacity of blob, which may be NULL to get *n_words only.
  *   Errors: HARTS_EINVAL (malformed forest, pages missing or negative, q_pos out of range, capacity), HARTS_ENOMEM.

@@ -88,8 +88,8 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
                 n_own++;
                 least = std::min<int64_t>(least, q_pos[x.row] + 1);
             }
-        const int64_t most = (int64_t)len[v] + (n_own ? grow : 0);
-        if (most >= INT32_MAX - TILE || page_ptr[v + 1] < page_ptr[v] || (most + page - 1) / page > page_ptr[v + 1] - page_ptr[v]) return HARTS_EINVAL;
+        const int64_t room = ((int64_t)page_ptr[v + 1] - page_ptr[v]) * page, most = std::min<int64_t>((int64_t)len[v] + (n_own ? grow : 0), room);
+        if (room < len[v] || most >= INT32_MAX - TILE) return HARTS_EINVAL;
         for (int32_t p = page_ptr[v]; p < page_ptr[v + 1]; p++) {
             if (pages[p] < 0) return HARTS_EINVAL;
             ix.max_page = std::max(ix.max_page, pages[p]);

@@ -123,17 +123,19 @@ GOOD = dict(tree_node_ptr=[0, 2], node_parent=[-1, 0], node_fork_off=[0, 10], no
 
 def test_the_good_one_is_taken():
     H.harts_gen_attn_index(**GOOD)
-    H.harts_gen_attn_index(**GOOD, grow=11)
+    for grow in (11, 12, 2 ** 31 - 1):              # as far as the pages go
+        entries = arrays(H.harts_gen_attn_index(**GOOD, grow=grow))[1]
+        assert {abs(x[3]) for x in entries if x[1] < 0} == {16}
     H.harts_gen_attn_index([0], [], [], [], [0], [], 16, [], [], 4, 2)
     H.harts_gen_attn_index([0], [], [], [], [0], [], 16, [-1], [0], 4, 2)
 
 
 @pytest.mark.parametrize("bad", [
-    dict(page=17), dict(page=8), dict(page=256), dict(Hq=3), dict(Hkv=0), dict(Hq=0), dict(grow=-1), dict(grow=12), dict(q_pos=[5]), dict(q_pos=[-2]),
+    dict(page=17), dict(page=8), dict(page=256), dict(Hq=3), dict(Hkv=0), dict(Hq=0), dict(grow=-1), dict(q_pos=[5]), dict(q_pos=[-2]),
     dict(q_node=[2]), dict(node_len=[10, -1]), dict(node_len=[17, 5]), dict(node_fork_off=[0, 11]), dict(node_fork_off=[0, -1]),
     dict(node_fork_off=[1, 10]), dict(node_parent=[0, 0]), dict(node_parent=[-1, 1]), dict(node_parent=[-1, -1]), dict(node_page=[3, -1]),
     dict(node_page_ptr=[0, 2, 2]), dict(node_page_ptr=[0, 3, 2]), dict(node_page_ptr=[1, 1, 2]), dict(tree_node_ptr=[0, 0, 2]), dict(q_pos=[4, 4]),
-    dict(grow=2 ** 31 - 1), dict(node_page=[3])])
+    dict(node_page=[3])])
 def test_what_is_refused(bad):
     with pytest.raises(H.HartsError) as e:
         H.harts_gen_attn_index(**{**GOOD, **bad})
