@@ -44,6 +44,7 @@ extern "C" {
  *   q, k [n_rows, H, dk], v [n_rows, H, dv] in `dtype`, heads contiguous, ld_q, ld_k, ld_v elements between rows (>= H d, a multiple
  *            of 16 bytes); g fp32 [n_rows, H], <= 0; o [n_rows, H, dv] contiguous, or NULL: only the states are wanted, q may be NULL
  *            then too.  Rows of no sequence are neither read nor written.
+ *            Sequences do not share rows, and o overlaps no input: what is written then is undefined.
  *   states fp32 [n_states, H, dk, dv]: the layout of the slots of harts_la.h, so that a training forward's slots can be the pool.
  *   workspace: harts_gen_la_workspace_bytes(), for chunked calls only (NULL where that is 0).  Calls that share it, also as parts of
  *            captured graphs, must not run at the same time.
@@ -107,7 +108,7 @@ int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache
  *   Errors: HARTS_EINVAL (malformed forest, pages missing or negative, q_pos out of range, capacity), HARTS_ENOMEM.
  * harts_gen_attn_workspace_bytes: of the parts of split sums.  Calls that share a workspace must not run at the same time.
  * harts_gen_attn: q bf16 [n_q, Hq, 128], heads contiguous, ld_q elements between rows; q_pos device int32 [n_q]; o bf16, lse fp32,
- *   contiguous, written for every query.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
+ *   contiguous, written for every query, neither overlapping an input.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
  *   Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
  */
 #define HARTS_GEN_ATTN_HEADER_WORDS 32

@@ -58,7 +58,7 @@ int32_t gen_cache_read(const GenCache& c, const GenRows& r);
 
 // Index of harts_gen_attn_index: header words, then the arrays (gen_attn_host.cc writes it, gen_attn.cu reads it).
 namespace gen_attn {
-enum Header { N_Q, HQ, HKV, PAGE, N_NARROW, N_WIDE, N_PARTS, MERGED, MAX_PAGE, WORDS, NARROW, WIDE, ENTRY, PAGES, PART_PTR, PART, NARROW_MAX, N_LISTS, LIST_PTR, BESIDE };
+enum Header { N_Q, HQ, HKV, PAGE, N_NARROW, N_WIDE, N_PARTS, MERGED, MAX_PAGE, WORDS, NARROW, WIDE, ENTRY, PAGES, PART_PTR, PART, NARROW_MAX, N_LISTS, LIST_PTR };
 constexpr int NARROW_ROWS = 16, WIDE_ROWS = 128;
 struct Unit {                 // rows that read the same tokens of a node: rows flat0 .. flat0 + n - 1 of (entry, head of the group)
     int32_t entry, flat0, n, k0, k1, page0, part0, pad;

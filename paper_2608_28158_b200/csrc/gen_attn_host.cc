@@ -33,7 +33,7 @@ struct Index {
     std::vector<Unit> narrow, wide;
     std::vector<Entry> entries;
     std::vector<int32_t> part_ptr, part, list_ptr;
-    int32_t n_parts = 0, merged = 0, max_page = -1, beside = 0;
+    int32_t n_parts = 0, merged = 0, max_page = -1;
 };
 
 bool forest_ok(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const int32_t* off, const int32_t* len) {
@@ -95,9 +95,9 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
             ix.max_page = std::max(ix.max_page, pages[p]);
         }
         if (s.empty()) continue;
-        // what its own queries see for certain, in whole tiles, is shared with the branches below; a node of few rows alone is one run
+        // what its own queries see for certain, in whole tiles and without the last token, is shared with the branches below; a node of few rows alone is one run
         int own_from = 0;
-        if (n_own && (n_own < (int)s.size() || (int64_t)n_own * G > NARROW_ROWS)) own_from = (int)(least / TILE * TILE);
+        if (n_own && (n_own < (int)s.size() || (int64_t)n_own * G > NARROW_ROWS)) own_from = least > 0 ? (int)((least - 1) / TILE * TILE) : 0;
         std::vector<int32_t> limits;
         for (Sees& x : s) {
             const int32_t l = x.limit < 0 ? own_from : x.limit;
@@ -159,7 +159,6 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
     // 16,421 tokens, 28 wide and 38 narrow tiles an SM: 80 -> 61 us).  A tile takes such a CTA 1.5 times what it takes the kernel alone, so
     // beyond 2 : 1 they run one after the other, each with the GPU to itself.
     const bool beside = wide_tiles > 0 && narrow_tiles <= 2 * wide_tiles && wide_tiles <= 2 * narrow_tiles;
-    ix.beside = beside;
     std::stable_sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.b - x.a > y.b - y.a; });
     std::vector<std::vector<int32_t>> parts(n_q);
     int64_t n_parts = 0;
@@ -282,7 +281,7 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
                                         const int32_t* node_fork_off, const int32_t* node_len, const int32_t* node_page_ptr,
                                         const int32_t* node_page, int32_t page, int32_t n_q, const int32_t* q_node, const int32_t* q_pos,
                                         int32_t Hq, int32_t Hkv, int32_t grow, int64_t cap_words, int32_t* blob, int64_t* n_words) {
-    if (n_trees < 0 || n_q < 0 || grow < 0 || !tree_node_ptr || !node_page_ptr || !n_words || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 ||
+    if (n_trees < 0 || n_q < 0 || grow < 0 || !tree_node_ptr || !node_page_ptr || !n_words || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 || (int64_t)n_q * Hq > INT32_MAX ||
         (page != 16 && page != 32 && page != 64 && page != 128))
         return HARTS_EINVAL;
     if (tree_node_ptr[0] != 0 || tree_node_ptr[n_trees] < 0 || node_page_ptr[0] != 0) return HARTS_EINVAL;
@@ -320,7 +319,6 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
         blob[WORDS] = (int32_t)total;
         for (const Unit& u : ix.narrow) blob[NARROW_MAX] = std::max(blob[NARROW_MAX], u.n);
         for (int i = 0; i < 6; i++) blob[NARROW + i] = (int32_t)at[i];
-        blob[BESIDE] = ix.beside;
         blob[N_LISTS] = std::max<int32_t>(0, (int32_t)ix.list_ptr.size() - 1);
         blob[LIST_PTR] = (int32_t)at[6];
         auto put = [&](int i, const void* p, int64_t words) {

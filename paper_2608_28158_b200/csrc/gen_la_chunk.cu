@@ -68,19 +68,38 @@ plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, in
         if (s.out < 0 && !(a.o && s.len > 0)) return make_int2(0, 0);
         return make_int2(s.len / rows, s.len == 0 || s.len % rows != 0);
     };
-    int whole = 0;
-    GenSeq s;
-    for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) whole += look_up(i0 + tid, s, true).x;
-    for (int d = 16; d > 0; d >>= 1) whole += __shfl_xor_sync(~0u, whole, d);
-    if (lane == 0) warp_sum[warp].x = whole;
+    GenSeq s, s0;
+    const int2 n0 = look_up(tid, s0, true);       // (kept: there are seldom more sequences than threads)
+    int2 all = n0;
+    for (int i0 = PLAN_THREADS; i0 < a.n_seq; i0 += PLAN_THREADS) {
+        const int2 n = look_up(i0 + tid, s, true);
+        all.x += n.x;
+        all.y += n.y;
+    }
+    for (int d = 16; d > 0; d >>= 1) {
+        all.x += __shfl_xor_sync(~0u, all.x, d);
+        all.y += __shfl_xor_sync(~0u, all.y, d);
+    }
+    if (lane == 0) warp_sum[warp] = all;
     __syncthreads();
-    whole = 0;
-    for (int w = 0; w < PLAN_THREADS / 32; w++) whole += warp_sum[w].x;
+    all = make_int2(0, 0);
+    for (int w = 0; w < PLAN_THREADS / 32; w++) {
+        all.x += warp_sum[w].x;
+        all.y += warp_sum[w].y;
+    }
     __syncthreads();
+    const int whole = all.x;
+    const bool fits = whole + all.y <= max_items;         // sequences that share rows can have more items than the rows allow: none of them is done
+    if (tid == 0) {
+        if (!fits) gen_report(a.dev_status, 0);
+        count[0] = fits ? whole + all.y : 0;
+        count[1] = 0;                             // the walk's counter
+    }
     int2 base = make_int2(0, whole);
     for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
-        const int2 n = look_up(i, s, false);
+        const int2 n = i0 == 0 ? n0 : look_up(i, s, false);
+        if (i0 == 0) s = s0;
         int2 upto = n;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -102,8 +121,7 @@ plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, in
             base.y += warp_sum[w].y;
         }
         const int items_here = n.x + n.y;
-        if (items_here > 0 && (whole > max_items || at.y + n.y > max_items)) {        // rows that sequences share: more items than the rows allow
-            gen_report(a.dev_status, i);
+        if (i < a.n_seq && !fits) {
             chains[i] = make_int4(0, 0, -1, -1);
         } else if (i < a.n_seq) {
             for (int j = 0; j < items_here; j++) {
@@ -115,10 +133,6 @@ plan_kernel(const GenLaArgs a, int L, int max_items, int* count, int4* items, in
             chains[i] = make_int4(at.x, items_here, s.in, n.y ? at.y : -1);
         }
         __syncthreads();
-    }
-    if (tid == 0) {
-        count[0] = whole > max_items ? 0 : min(base.y, max_items);
-        count[1] = 0;                             // the walk's counter
     }
 }
 

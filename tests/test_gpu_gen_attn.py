@@ -311,7 +311,7 @@ def test_positions_out_of_range_are_brought_in_and_reported():
     q_node, q_pos = [1, 2], [69, 129]
     index = tree.index(q_node, q_pos, 4)
     q = queries(2, 4, 8)
-    for r, bad, used in ((1, 140, 139), (0, 80, 79), (0, 2 ** 31 - 1, 79)):
+    for r, bad, used in ((1, 140, 139), (0, 80, 79), (0, 2 ** 31 - 1, 79), (0, 68, 69), (1, -1, 129), (1, -2 ** 31, 129)):
         pos = list(q_pos)
         pos[r] = bad
         o, lse, status = run(tree, index, q, pos, 0.1)
@@ -363,3 +363,41 @@ def test_queries_of_any_size(scale):
     for kind in KINDS:
         tree = Tree([0, 1], [-1], [0], [200], 32, 2, kind, 30)
         check(tree, [0, 0], [150, 199], 4, 30, q_scale=scale, scale=0.1 / scale)
+
+
+@pytest.mark.parametrize("drafts,n", [(8, 640), (8, 641), (3, 64)])
+def test_positions_below_the_index_s_are_reported_by_shared_runs_too(drafts, n):
+    tree = Tree([0, 1], [-1], [0], [n], 64, 1, "bf16", 12)
+    q_pos = [n - 1] * drafts
+    index = tree.index([0] * drafts, q_pos, 8)
+    q = queries(drafts, 8, 12)
+    o, lse, status = run(tree, index, q, [n - 1] * (drafts - 1) + [n - 2], 0.1)
+    with pytest.raises(H.HartsError):
+        H.harts_la_check(status)
+    assert int(status[1]) == drafts - 1
+    compare(o, lse, *tree.oracle(q, [0] * drafts, q_pos, 0.1))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [1, 5])
+def test_pages_far_into_a_large_cache(kind, rows):
+    """Places beyond 2^32 bytes and elements."""
+    n_pages, hkv, page, n = 70000, 4, 128, 300
+    dt = torch.float8_e4m3fn if kind == "e4m3" else torch.bfloat16
+    cache = [torch.zeros(n_pages, hkv, page, 128, dtype=dt, device="cuda") for _ in range(2)]
+    exps = [torch.full((n_pages, hkv, page), 120, dtype=torch.uint8, device="cuda") if kind == "e4m3" else None for _ in range(2)]
+    pages = [n_pages - 1, n_pages // 2 + 1, n_pages - 7]
+    kv = [torch.randn(n, hkv, 128, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    slot = torch.tensor([pages[j // page] * page + j % page for j in range(n)], dtype=torch.int32, device="cuda")
+    H.harts_gen_cache_write(*kv, slot, *cache, *exps)
+    H.harts_gen_cache_read(*cache, slot, *kv, *exps)
+    q_node, q_pos = [0] * rows, [n - 1 - i for i in range(rows)]
+    index = H.harts_gen_attn_index([0, 1], [-1], [0], [n], [0, 3], pages, page, q_node, q_pos, 16 * hkv, hkv).upload()
+    q = queries(rows, 16 * hkv, 1)
+    o, lse = torch.empty_like(q), torch.empty(rows, 16 * hkv, device="cuda")
+    ws = torch.empty(max(16, index.workspace_bytes), dtype=torch.uint8, device="cuda")
+    H.harts_gen_attn(index, q, *cache, torch.tensor(q_pos, dtype=torch.int32, device="cuda"), o, lse, 0.1, ws, *exps)
+    for r, p in enumerate(q_pos):
+        s = torch.einsum("hgd,thd->hgt", q[r].double().view(hkv, 16, 128), kv[0][:p + 1].double()) * 0.1
+        ref = torch.einsum("hgt,thd->hgd", torch.softmax(s, -1), kv[1][:p + 1].double()).reshape(-1, 128)
+        assert float((o[r].double() - ref).norm() / ref.norm()) <= 2.0 ** -8

@@ -257,3 +257,14 @@ def test_the_framework_s_own_forward_gives_the_same_outputs():
     o, status = call(q, k, v, g, states, begin, lens, [-1] * 3, [-1] * 3)
     H.harts_la_check(status)
     assert rel(o, ref[rows]) <= 2.0 ** -8
+
+
+def test_sequences_that_share_rows_beyond_the_workspace_are_refused_on_the_device():
+    """Twelve sequences of the same 4,000 rows: more segments than 4,000 rows can have.  None is done, and the call says so."""
+    q, k, v, g, states, _, _, _ = problem([4000], 8, 128, "bf16", 11)
+    pool = torch.zeros(13, 8, 128, 128, device="cuda")
+    o, status = call(q, k, v, g, pool, [0] * 12, [4000] * 12, [-1] * 12, list(range(12)))
+    with pytest.raises(H.HartsError) as e:
+        H.harts_la_check(status)
+    assert e.value.code == -1
+    assert bool(torch.isnan(o).all()) and not pool.any()
