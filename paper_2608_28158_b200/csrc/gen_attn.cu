@@ -485,29 +485,33 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
     after_previous();                                     // (the wide kernel ran beside this one; the merge waits for this one only)
 }
 
-// A query head's parts joined: one warp each, four elements a lane.  Queries of one part have been written by their unit.
+// A query head's parts joined: W warps, four elements a lane.  Queries of one part have been written by their unit.  One warp a head where
+// that gives every scheduler one, else four, a quarter of the parts each (3 x 32 heads of 75 parts 12 -> 9 us; 280 x 16 heads the other way, 17
+// against 13).
 constexpr int MERGE_WARPS = 4;
+template <int W>
 __global__ void __launch_bounds__(MERGE_WARPS * 32)
 merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __restrict__ part_lse, __nv_bfloat16* __restrict__ o, float* __restrict__ lse) {
-    const int64_t out = (int64_t)blockIdx.x * MERGE_WARPS + (threadIdx.x >> 5);
-    if (out >= (int64_t)t.n_q * t.Hq) {
+    __shared__ float4 so[W][32];
+    __shared__ float2 stats[W];
+    const int64_t out = (int64_t)blockIdx.x * (MERGE_WARPS / W) + (W == 1 ? threadIdx.x >> 5 : 0);
+    if (out >= (int64_t)t.n_q * t.Hq) {           // (a whole warp)
         after_previous();
         return;
     }
-    const int lane = threadIdx.x & 31, row = (int)(out / t.Hq), head = (int)(out % t.Hq), G = t.Hq / t.Hkv, h = head / G, g = head % G;
+    const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, row = (int)(out / t.Hq), head = (int)(out % t.Hq), G = t.Hq / t.Hkv, h = head / G,
+              g = head % G;
     // (the index is the call's input: only the parts are the previous kernels')
-    const int p0 = t.part_ptr[row], p1 = t.part_ptr[row + 1];
-    int at = p0 + lane < p1 ? t.part[p0 + lane] + g : -1;
+    const int p0 = t.part_ptr[row], p1 = t.part_ptr[row + 1], n = (p1 - p0 - warp + W - 1) / W;       // this warp's: every W-th
+    auto place = [&](int i) { return i < n ? t.part[p0 + warp + W * i] + g : -1; };
+    int at = place(lane);
     after_previous();
     if (p1 == p0 + 1) return;
     float M = -INFINITY, L = 0.f;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    bool nan = false;
-    for (int b = p0; b < p1; b += 32) {           // 32 parts at a time: a lane has a part's place and weight
-        const int n = min(32, p1 - b);
-        if (b > p0) at = lane < n ? t.part[b + lane] + g : -1;
-        const float l = lane < n ? part_lse[(int64_t)at * t.Hkv + h] : -INFINITY;
-        nan |= l != l;
+    for (int b = 0; b < n; b += 32) {             // 32 parts at a time: a lane has a part's place and weight
+        if (b > 0) at = place(b + lane);
+        const float l = b + lane < n ? part_lse[(int64_t)at * t.Hkv + h] : -INFINITY;
         float m = l;
 #pragma unroll
         for (int x = 1; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, x));
@@ -520,9 +524,10 @@ merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __re
             y.w *= f;
             M = m;
         }
-        const float w = M == -INFINITY ? 0.f : ex2(l - M);
+        const float w = l != l ? l : M == -INFINITY ? 0.f : ex2(l - M);
+        const int here = min(32, n - b);
 #pragma unroll 8
-        for (int i = 0; i < n; i++) {
+        for (int i = 0; i < here; i++) {
             const float wi = __shfl_sync(~0u, w, i);
             const float4 z = *reinterpret_cast<const float4*>(part_o + ((int64_t)__shfl_sync(~0u, at, i) * t.Hkv + h) * D + 4 * lane);
             L += wi;
@@ -533,11 +538,32 @@ merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __re
             y.w += wi * z.w;
         }
     }
-    nan = __any_sync(~0u, nan);
-    const bool none = M == -INFINITY && !nan;
-    const float inv = none ? 0.f : nan ? __uint_as_float(0x7fffffffu) : 1.f / L;
+    if constexpr (W > 1) {
+        so[warp][lane] = y;
+        if (lane == 0) stats[warp] = make_float2(M, L);
+        __syncthreads();
+        if (warp != 0) return;
+#pragma unroll
+        for (int x = 0; x < W; x++) M = fmaxf(M, stats[x].x);
+        L = 0.f;
+        y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int x = 0; x < W; x++) {
+            const float2 part = stats[x];
+            if (part.y == 0.f) continue;          // (NaN goes on)
+            const float f = part.x == -INFINITY ? 1.f : ex2(part.x - M);
+            const float4 z = so[x][lane];
+            L += f * part.y;
+            y.x += f * z.x;
+            y.y += f * z.y;
+            y.z += f * z.z;
+            y.w += f * z.w;
+        }
+    }
+    const bool none = L == 0.f;
+    const float inv = none ? 0.f : 1.f / L;
     *reinterpret_cast<uint2*>(o + out * D + 4 * lane) = make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-    if (lane == 0) lse[out] = none ? -INFINITY : nan ? inv : (M + log2f(L)) * LN2;
+    if (lane == 0) lse[out] = none ? -INFINITY : (M + log2f(L)) * LN2;
 }
 
 template <bool F8, int NR>
@@ -589,9 +615,10 @@ int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int
         if ((rc = narrow(t, hi[N_LISTS], a, hi[N_WIDE] > 0)) != HARTS_OK) return rc;
     }
     if (hi[MERGED]) {
-        const int64_t blocks = ((int64_t)t.n_q * t.Hq + MERGE_WARPS - 1) / MERGE_WARPS;
-        if (blocks > INT32_MAX) return HARTS_EINVAL;
-        if (launch_after(merge_kernel, (int)blocks, MERGE_WARPS * 32, 0, st, t, (const float*)part_o, (const float*)part_lse, (__nv_bfloat16*)o, lse) != cudaSuccess)
+        const int heads = t.n_q * t.Hq;           // (it fits: the index saw to it)
+        const bool few = heads <= 4 * sm_count();
+        if (launch_after(few ? merge_kernel<4> : merge_kernel<1>, few ? heads : (int)(((int64_t)heads + MERGE_WARPS - 1) / MERGE_WARPS), MERGE_WARPS * 32, 0, st, t,
+                         (const float*)part_o, (const float*)part_lse, (__nv_bfloat16*)o, lse) != cudaSuccess)
             return HARTS_ECUDA;
     }
     return HARTS_OK;
