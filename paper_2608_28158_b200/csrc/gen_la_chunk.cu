@@ -1,7 +1,7 @@
 // Linear attention from and into kept states in chunks (bf16, d = 128): the work table, and what lets several CTAs share one long
 // sequence.
 //
-// The walk itself is pipe_fwd_kernel (la_pipe_fwd.cu): 1.5 us a chunk and head where the chain of chunks is what counts.  A sequence that
+// The walk itself is pipe_fwd_kernel (la_pipe_fwd.cu): 2.2 us a chunk and head where the chain of chunks is what counts.  A sequence that
 // is long beside what every SM has to do is cut into segments of L chunks, whose start states are found first:
 //     U_i = sum over segment i of e^{B_end - B_j} k_j^T v_j,   S_{i+1} = e^{B_i} S_i + U_i
 // The sums do not depend on each other (one product of k~^T v with the tokens as its inner dimension, left in tensor memory until the
@@ -37,7 +37,9 @@ Sizes sizes_of(const GenLaArgs& a) {
     z.L = 0;
     if (longest > 8 && 2 * longest > 3 * share) {
         const int64_t L = room > 0 ? (chunks + room - 1) / room : (share + 1) / 2;
-        z.L = (int)(L < 4 ? 4 : L > MAX_L ? MAX_L : L);
+        // A chunk takes a walk 2.2 us, its part of a sum 1.5, and the two passes' own time is that of some six chunks: a cut has to be worth that
+        // (16 sequences of 16 chunks x 4 heads: in segments of 13 70 us, whole 45).
+        if (4 * longest > 7 * L + 24) z.L = (int)(L < 4 ? 4 : L > MAX_L ? MAX_L : L);
     }
     z.max_items = a.n_seq + (z.L ? chunks / z.L : 0);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };

@@ -144,12 +144,37 @@ __device__ __forceinline__ void mma_lo(uint32_t d, uint32_t a, uint32_t b, uint3
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\tsetp.ne.b32 p, %5, 0;\n\t"
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(DESC_HI), "r"(idesc), "n"(ADD ? 1 : 0) : "memory");
 }
+__device__ __forceinline__ void mma_first(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    if (add) mma_lo<true>(d, a, b, idesc);
+    else mma_lo<false>(d, a, b, idesc);
+}
 // d (+)= sum over k-steps; the lower words advance by SA, SB a step, by GA more behind the fourth (K contiguous: the next panel)
-template <int STEPS, int SA, int SB, int GA, int GB, bool ADD = false>
+template <int STEPS, int SA, int SB, int GA, int GB>
 __device__ __forceinline__ void mma_steps(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
-    mma_lo<ADD>(d, a, b, idesc);
+    mma_lo<false>(d, a, b, idesc);
 #pragma unroll
     for (int ks = 1; ks < STEPS; ks++) mma_lo<true>(d, a + ks * SA + (ks >> 2) * GA, b + ks * SB + (ks >> 2) * GB, idesc);
+}
+
+// Rows from .. to - 1 of a panel of keys, weighted, as three terms: over the rows, and in two tiles behind each other.  Rows from `valid` on are
+// others' and become zeros.  One copy of the code for the roles that call it, and a small one (see the note on instruction memory above).
+static __device__ __noinline__ void weigh_rows(unsigned char* sk, unsigned char* sl, const uint2* w, int from, int to, int valid) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int t = from + (lane >> 3); t < to; t += 4) {
+        const uint32_t off = sw128_chunk(t, lane & 7);
+        const float f = __uint_as_float(w[t].x);
+        const F2 w2 = f2(f, f);
+        uint4 y = *reinterpret_cast<const uint4*>(sk + off), z, z2;
+        if (t >= valid) y = make_uint4(0, 0, 0, 0);
+        three_terms(y.x, z.x, z2.x, w2);
+        three_terms(y.y, z.y, z2.y, w2);
+        three_terms(y.z, z.z, z2.z, w2);
+        three_terms(y.w, z.w, z2.w, w2);
+        *reinterpret_cast<uint4*>(sk + off) = y;
+        *reinterpret_cast<uint4*>(sl + off) = z;
+        *reinterpret_cast<uint4*>(sl + 2 * PANEL + off) = z2;
+    }
 }
 
 template <int NV, bool GEN>
@@ -335,7 +360,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
 #pragma unroll
             for (int u = 0; u < 8; u++)
                 if (!GEN || u < 4) *reinterpret_cast<uint4*>(smem + S::p + (u >> 2) * PANEL + sw128_chunk(t, 4 + (u & 3))) = make_uint4(0, 0, 0, 0);
-        // GEN: rows from .. to - 1 of a panel of weighted keys, as three terms.  The warps that mask take a quarter of them.
+        // GEN: rows from .. to - 1 of a panel of weighted keys, as three terms.  The warps that mask take half of them.
         bool added = false;                       // there is a sum before this chunk's
         auto weigh = [&](const Record& rd, int panel, int from, int to) {
             if (!rd.step) return true;
@@ -345,30 +370,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 rl.next();
             }
             added = true;
-            unsigned char *sk = smem + rg.i * S::STAGE + S::K + panel * PANEL, *sl = smem + S::lo + panel * PANEL;
-#pragma unroll 1
-            for (int t0 = from + (lane >> 3); t0 < to; t0 += 16) {
-                uint4 y[4];
-                float w[4];
-#pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    y[u] = *reinterpret_cast<const uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7));
-                    w[u] = __uint_as_float(rd.w[t0 + 4 * u].x);
-                    if (t0 + 4 * u >= rd.valid) y[u] = make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    uint4 z, z2;
-                    const F2 w2 = f2(w[u], w[u]);
-                    three_terms(y[u].x, z.x, z2.x, w2);
-                    three_terms(y[u].y, z.y, z2.y, w2);
-                    three_terms(y[u].z, z.z, z2.z, w2);
-                    three_terms(y[u].w, z.w, z2.w, w2);
-                    *reinterpret_cast<uint4*>(sk + sw128_chunk(t0 + 4 * u, lane & 7)) = y[u];
-                    *reinterpret_cast<uint4*>(sl + sw128_chunk(t0 + 4 * u, lane & 7)) = z;
-                    *reinterpret_cast<uint4*>(sl + 2 * PANEL + sw128_chunk(t0 + 4 * u, lane & 7)) = z2;
-                }
-            }
+            weigh_rows(smem + rg.i * S::STAGE + S::K + panel * PANEL, smem + S::lo + panel * PANEL, rd.w, from, to, rd.valid);
             return true;
         };
         for (;;) {
@@ -377,7 +379,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
             if (rd.end) break;
             if (quarter < 2) {                    // P = A .* decay: lanes 0..63 hold the rows
                 if constexpr (GEN) {
-                    if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph) || !weigh(rd, quarter, 48, 64)) break;
+                    if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph) || !weigh(rd, quarter, 32, 64)) break;
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&m.ready[ra.i]);
@@ -436,7 +438,7 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if (!wait_both(&m.full[rg.i], rg.ph, &m.a_full[ra.i], ra.ph)) break;
                 if constexpr (GEN) {
                     const int valid = rd.valid;
-                    if (!weigh(rd, quarter - 2, 0, 48)) break;
+                    if (!weigh(rd, quarter - 2, 0, 32)) break;
                     if (valid < BT && quarter - 2 < VP) {
                         unsigned char* sv = smem + rg.i * S::STAGE + S::V + (quarter - 2) * PANEL;
 #pragma unroll 1
@@ -686,11 +688,17 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 tc_fence_after();
                 if (step) {
                     if (elect_one()) {
-                        mma_steps<4, MN, MN, 0, 0>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(tile + S::K), desc_lo_mn<BT>(tile + S::V), IDESC_U);
-                        if constexpr (GEN)
+                        if constexpr (GEN) {
+#pragma unroll 1
+                            for (int term = 0; term < 3; term++) {
+                                const uint32_t a = desc_lo_mn<BT>(term == 0 ? tile + S::K : base + S::lo + (term - 1) * 2 * PANEL), b = desc_lo_mn<BT>(tile + S::V);
+                                mma_first(tmem + S::COL_U + ru.i * NV, a, b, IDESC_U, term > 0);
 #pragma unroll
-                            for (int term = 0; term < 2; term++)
-                                mma_steps<4, MN, MN, 0, 0, true>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(base + S::lo + term * 2 * PANEL), desc_lo_mn<BT>(tile + S::V), IDESC_U);
+                                for (int ks = 1; ks < 4; ks++) mma_lo<true>(tmem + S::COL_U + ru.i * NV, a + ks * MN, b + ks * MN, IDESC_U);
+                            }
+                        } else {
+                            mma_steps<4, MN, MN, 0, 0>(tmem + S::COL_U + ru.i * NV, desc_lo_mn<BT>(tile + S::K), desc_lo_mn<BT>(tile + S::V), IDESC_U);
+                        }
                         mma_commit(&m.u_full[ru.i]);
                     }
                     __syncwarp();
