@@ -39,9 +39,19 @@ __device__ __forceinline__ int64_t row_at(const GenCache& c, int slot, int h) {
     const int shift = 31 - __clz(c.page);
     return ((int64_t)(slot >> shift) * c.Hkv + h) * c.page + (slot & (c.page - 1));
 }
-// A CTA has PER * 32 tokens of one head (of k or of v), so that rows of a page that follow each other are written by one CTA; a thread has PER
-// rows, whose loads are on their way together.
-constexpr int PER = 2, TOKENS = PER * NT / LANES;
+// A CTA has 32 rows of k or of v in their own order, (token, head), so that what it reads (or writes) of them is in one piece; one row a
+// thread.  A CTA for one head of 64 tokens, whose pages' rows follow each other instead: 16,385 tokens x 8 heads written in 24.8 us instead
+// of 22.8, 24,000 x 4 read in 20.7 instead of 18.7.  Two rows a thread: 22.7 and 21.2.
+constexpr int ROWS = NT / LANES;
+struct Place {
+    int64_t token;
+    int h;
+};
+__device__ __forceinline__ Place place_of(const GenCache& c) {
+    const int64_t id = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (id <= UINT32_MAX) return {(uint32_t)id / (uint32_t)c.Hkv, (int)((uint32_t)id % (uint32_t)c.Hkv)};
+    return {id / c.Hkv, (int)(id % c.Hkv)};
+}
 // The slot of a token, -1: none.  The first lane of the token's first head reports one beyond the cache.
 __device__ __forceinline__ int slot_of(const GenCache& c, const GenRows& r, int64_t token, bool report) {
     if (token >= r.n) return -1;
@@ -54,115 +64,95 @@ __device__ __forceinline__ int slot_of(const GenCache& c, const GenRows& r, int6
 
 template <bool F8>
 __global__ void __launch_bounds__(NT) write_kernel(const GenCache c, const GenRows r) {
-    const int lane = threadIdx.x % LANES, h = blockIdx.y;
-    const bool is_v = blockIdx.z != 0;
-    int slot[PER];
-    uint4 x[PER][2];
-#pragma unroll
-    for (int i = 0; i < PER; i++) {
-        const int64_t token = (int64_t)blockIdx.x * TOKENS + i * (NT / LANES) + threadIdx.x / LANES;
-        slot[i] = slot_of(c, r, token, lane == 0 && h == 0 && !is_v);
-        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-        if (slot[i] >= 0) {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_v ? r.v : r.k) + token * (is_v ? r.ld_v : r.ld_k) + h * D + lane * 16;
-            x[i][0] = *reinterpret_cast<const uint4*>(src);
-            x[i][1] = *reinterpret_cast<const uint4*>(src + 8);
-        }
+    const int lane = threadIdx.x % LANES;
+    const bool is_v = blockIdx.y != 0;
+    const Place at = place_of(c);
+    const int slot = slot_of(c, r, at.token, lane == 0 && at.h == 0 && !is_v);
+    uint4 x[2] = {};
+    if (slot >= 0) {
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_v ? r.v : r.k) + at.token * (is_v ? r.ld_v : r.ld_k) + (int64_t)at.h * D + lane * 16;
+        x[0] = *reinterpret_cast<const uint4*>(src);
+        x[1] = *reinterpret_cast<const uint4*>(src + 8);
     }
+    const int64_t row = slot >= 0 ? row_at(c, slot, at.h) : 0;
+    if constexpr (!F8) {
+        if (slot < 0) return;
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(is_v ? c.v : c.k) + row * D + lane * 16);
+        dst[0] = x[0];
+        dst[1] = x[1];
+    } else {
+        uint32_t top = top_of(x);                          // bits of bf16 magnitudes are in the order of the magnitudes
 #pragma unroll
-    for (int i = 0; i < PER; i++) {
-        const int64_t row = slot[i] >= 0 ? row_at(c, slot[i], h) : 0;
-        if constexpr (!F8) {
-            if (slot[i] < 0) continue;
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(is_v ? c.v : c.k) + row * D + lane * 16);
-            dst[0] = x[i][0];
-            dst[1] = x[i][1];
-        } else {
-            uint32_t top = top_of(x[i]);                   // bits of bf16 magnitudes are in the order of the magnitudes
+        for (int m = 1; m < LANES; m <<= 1) top = max(top, __shfl_xor_sync(~0u, top, m));
+        if (slot < 0) return;
+        // 448 = 1.75 2^8: the power goes one up where the significand is above 1.75
+        const int exp = top >= 0x7f80u ? 255 : max((int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u), 1);
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (exp != 255) {
+            uint32_t w[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+            if (exp == 247) {                              // 256 2^120 would not be a number any more: the next one below it is taken
 #pragma unroll
-            for (int m = 1; m < LANES; m <<= 1) top = max(top, __shfl_xor_sync(~0u, top, m));
-            if (slot[i] < 0) continue;
-            // 448 = 1.75 2^8: the power goes one up where the significand is above 1.75
-            const int exp = top >= 0x7f80u ? 255 : max((int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u), 1);
-            uint4 y = make_uint4(0, 0, 0, 0);
-            if (exp != 255) {
-                uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
-                if (exp == 247) {                          // 256 2^120 would not be a number any more: the next one below it is taken
-#pragma unroll
-                    for (int e = 0; e < 8; e++) w[e] = (w[e] & 0x80008000u) | __vminu2(w[e] & 0x7fff7fffu, 0x7f707f70u);
-                }
-                const float f = __uint_as_float((uint32_t)(254 - exp) << 23);
-                y.x = two_e4m3(w[0], f) | two_e4m3(w[1], f) << 16;
-                y.y = two_e4m3(w[2], f) | two_e4m3(w[3], f) << 16;
-                y.z = two_e4m3(w[4], f) | two_e4m3(w[5], f) << 16;
-                y.w = two_e4m3(w[6], f) | two_e4m3(w[7], f) << 16;
+                for (int e = 0; e < 8; e++) w[e] = (w[e] & 0x80008000u) | __vminu2(w[e] & 0x7fff7fffu, 0x7f707f70u);
             }
-            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(is_v ? c.v : c.k) + row * D + lane * 16) = y;
-            if (lane == 0) (is_v ? c.v_exp : c.k_exp)[row] = (uint8_t)exp;
+            const float f = __uint_as_float((uint32_t)(254 - exp) << 23);
+            y.x = two_e4m3(w[0], f) | two_e4m3(w[1], f) << 16;
+            y.y = two_e4m3(w[2], f) | two_e4m3(w[3], f) << 16;
+            y.z = two_e4m3(w[4], f) | two_e4m3(w[5], f) << 16;
+            y.w = two_e4m3(w[6], f) | two_e4m3(w[7], f) << 16;
         }
+        *reinterpret_cast<uint4*>(static_cast<uint8_t*>(is_v ? c.v : c.k) + row * D + lane * 16) = y;
+        if (lane == 0) (is_v ? c.v_exp : c.k_exp)[row] = (uint8_t)exp;
     }
 }
 
 template <bool F8>
 __global__ void __launch_bounds__(NT) read_kernel(const GenCache c, const GenRows r) {
-    const int lane = threadIdx.x % LANES, h = blockIdx.y;
-    const bool is_v = blockIdx.z != 0;
+    const int lane = threadIdx.x % LANES;
+    const bool is_v = blockIdx.y != 0;
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(is_v ? r.v : r.k);
     if (!out) return;
-    int64_t token[PER];
-    int exp[PER];
-    uint4 x[PER][2];
-#pragma unroll
-    for (int i = 0; i < PER; i++) {
-        token[i] = (int64_t)blockIdx.x * TOKENS + i * (NT / LANES) + threadIdx.x / LANES;
-        const int slot = slot_of(c, r, token[i], lane == 0 && h == 0);
-        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-        exp[i] = 127;
-        if (slot >= 0) {
-            const int64_t row = row_at(c, slot, h);
-            if constexpr (F8) {
-                x[i][0] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + row * D + lane * 16);
-                exp[i] = (is_v ? c.v_exp : c.k_exp)[row];
-            } else {
-                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(is_v ? c.v : c.k) + row * D + lane * 16);
-                x[i][0] = src[0];
-                x[i][1] = src[1];
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; i++) {
-        if (token[i] >= r.n) continue;
+    const Place at = place_of(c);
+    if (at.token >= r.n) return;
+    const int slot = slot_of(c, r, at.token, lane == 0 && at.h == 0);
+    uint4 x[2] = {};
+    if (slot >= 0) {
+        const int64_t row = row_at(c, slot, at.h);
         if constexpr (F8) {
-            const float f = gen_power(exp[i]);
-            const uint32_t w[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
-            uint32_t z[8];
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                z[2 * e] = two_bf16(w[e], f);
-                z[2 * e + 1] = two_bf16(w[e] >> 16, f);
-            }
-            x[i][0] = make_uint4(z[0], z[1], z[2], z[3]);
-            x[i][1] = make_uint4(z[4], z[5], z[6], z[7]);
+            const uint4 y = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(is_v ? c.v : c.k) + row * D + lane * 16);
+            const float f = gen_power((is_v ? c.v_exp : c.k_exp)[row]);
+            x[0] = make_uint4(two_bf16(y.x, f), two_bf16(y.x >> 16, f), two_bf16(y.y, f), two_bf16(y.y >> 16, f));
+            x[1] = make_uint4(two_bf16(y.z, f), two_bf16(y.z >> 16, f), two_bf16(y.w, f), two_bf16(y.w >> 16, f));
+        } else {
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(is_v ? c.v : c.k) + row * D + lane * 16);
+            x[0] = src[0];
+            x[1] = src[1];
         }
-        uint4* dst = reinterpret_cast<uint4*>(out + (token[i] * c.Hkv + h) * D + lane * 16);
-        dst[0] = x[i][0];
-        dst[1] = x[i][1];
     }
+    uint4* dst = reinterpret_cast<uint4*>(out + (at.token * c.Hkv + at.h) * D + lane * 16);
+    dst[0] = x[0];
+    dst[1] = x[1];
 }
 
-dim3 grid_of(const GenCache& c, const GenRows& r) { return dim3((unsigned)((r.n + TOKENS - 1) / TOKENS), (unsigned)c.Hkv, 2); }
+int32_t grid_of(const GenCache& c, const GenRows& r, dim3& grid) {
+    const int64_t blocks = (r.n * c.Hkv + ROWS - 1) / ROWS;
+    grid = dim3((unsigned)blocks, 2);
+    return blocks <= INT32_MAX ? HARTS_OK : HARTS_EINVAL;
+}
 
 }  // namespace
 
 int32_t gen_cache_write(const GenCache& c, const GenRows& r) {
-    if (c.type == HARTS_E4M3) write_kernel<true><<<grid_of(c, r), NT, 0, r.stream>>>(c, r);
-    else write_kernel<false><<<grid_of(c, r), NT, 0, r.stream>>>(c, r);
+    dim3 grid;
+    if (grid_of(c, r, grid) != HARTS_OK) return HARTS_EINVAL;
+    if (c.type == HARTS_E4M3) write_kernel<true><<<grid, NT, 0, r.stream>>>(c, r);
+    else write_kernel<false><<<grid, NT, 0, r.stream>>>(c, r);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
 int32_t gen_cache_read(const GenCache& c, const GenRows& r) {
-    if (c.type == HARTS_E4M3) read_kernel<true><<<grid_of(c, r), NT, 0, r.stream>>>(c, r);
-    else read_kernel<false><<<grid_of(c, r), NT, 0, r.stream>>>(c, r);
+    dim3 grid;
+    if (grid_of(c, r, grid) != HARTS_OK) return HARTS_EINVAL;
+    if (c.type == HARTS_E4M3) read_kernel<true><<<grid, NT, 0, r.stream>>>(c, r);
+    else read_kernel<false><<<grid, NT, 0, r.stream>>>(c, r);
     return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
 }
 
