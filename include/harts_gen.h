@@ -42,7 +42,7 @@ extern "C" {
  *   max_len: host; a bound on the lengths.  It and n_rows choose the form: tokens one by one with the state in registers, or chunks
  *            of 64 on the tensor cores.
  *   q, k [n_rows, H, dk], v [n_rows, H, dv] in `dtype`, heads contiguous, ld_q, ld_k, ld_v elements between rows (>= H d, a multiple
- *            of 16 bytes); g fp32 [n_rows, H], <= 0; o [n_rows, H, dv] contiguous, or NULL: only the states are wanted, q may be NULL
+ *            of 16 bytes); g fp32 [n_rows, H], <= 0 (minus infinity too: the state is forgotten); o [n_rows, H, dv] contiguous, or NULL: only the states are wanted, q may be NULL
  *            then too.  Rows of no sequence are neither read nor written.
  *            Sequences do not share rows, and o overlaps no input: what is written then is undefined.
  *   states fp32 [n_states, H, dk, dv]: the layout of the slots of harts_la.h, so that a training forward's slots can be the pool.
@@ -51,6 +51,7 @@ extern "C" {
  * Served: fp32 with dk = dv = 64 or 128, bf16 with dk = dv = 64 or 128; chunks on the tensor cores for bf16 with 128, the others
  * walk token by token whatever their length.  States are fp32 and so are all sums; on the tensor cores the weighted keys are three bf16 terms each, so
  * that states keep fp32's accuracy, while scores and the states that outputs are made of are rounded to bf16, as in harts_la.h.
+ * There, an infinity or a NaN in a row's k or v can also reach the outputs (not the states) of the rows ahead of it in its chunk.
  * A sequence with a bad entry is left out (dev_status[1] = its number).
  * Errors: HARTS_EINVAL (null or misaligned pointer, size out of range, workspace too small), HARTS_EUNSUPPORTED, HARTS_ECUDA.
  */
@@ -109,7 +110,7 @@ int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache
  * harts_gen_attn_workspace_bytes: of the parts of split sums.  Calls that share a workspace must not run at the same time.
  * harts_gen_attn: q bf16 [n_q, Hq, 128], heads contiguous, ld_q elements between rows; q_pos device int32 [n_q]; o bf16, lse fp32,
  *   contiguous, written for every query, neither overlapping an input.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
- *   Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
+ *   scale is positive and finite.  Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
  */
 #define HARTS_GEN_ATTN_HEADER_WORDS 32
 int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_node_ptr, const int32_t* node_parent, const int32_t* node_fork_off,

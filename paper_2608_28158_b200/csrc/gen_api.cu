@@ -1,4 +1,6 @@
 // C entry points of sampling on rollout trees: argument checks and the choice of the kernel.
+#include <cfloat>
+
 #include "gen.h"
 
 namespace {
@@ -134,7 +136,7 @@ int32_t harts_gen_attn(const int32_t* host_index, const int32_t* dev_index, cons
                        int32_t* dev_status, void* stream) {
     using namespace harts::gen_attn;
     size_t need = 0;
-    if (harts_gen_attn_workspace_bytes(host_index, &need) != HARTS_OK || !dev_index || !aligned16(dev_index) || !(scale > 0.f)) return HARTS_EINVAL;
+    if (harts_gen_attn_workspace_bytes(host_index, &need) != HARTS_OK || !dev_index || !aligned16(dev_index) || !(scale > 0.f && scale <= FLT_MAX)) return HARTS_EINVAL;
     const int32_t rc = cache_check(host_index[N_Q], n_pages, host_index[PAGE], host_index[HKV], 128, cache_type);
     if (rc != HARTS_OK) return rc;
     if (host_index[N_Q] == 0) return HARTS_OK;

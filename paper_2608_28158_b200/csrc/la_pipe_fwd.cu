@@ -798,6 +798,10 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 if (c < 0) continue;
                 asm volatile("cp.async.wait_group 5;" ::: "memory");
                 float y[2] = {m.raw[c % RAW][lane] * LOG2E, m.raw[c % RAW][lane + 32] * LOG2E};
+                if constexpr (GEN) {              // 2^-150 is 0 already; differences of sums of infinities, or of very large terms, would be lost
+#pragma unroll
+                    for (int u = 0; u < 2; u++) y[u] = y[u] < -150.f ? -150.f : y[u];
+                }
                 float z[2] = {y[0], y[1]};        // GEN: what decays a row's key until the chunk's end, summed from there (a difference of
                 if constexpr (GEN) {              // running sums would lose it behind a strong decay)
 #pragma unroll

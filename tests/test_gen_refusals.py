@@ -136,3 +136,8 @@ def test_tensors_of_the_host_are_refused():
         H.harts_gen_cache_read(c, c, i, x, x)
     with pytest.raises(H.HartsError):
         H.harts_gen_attn(index(), x, c, c, i, x, torch.zeros(3, 4), 0.1)
+
+
+def test_attn_refuses_an_infinite_scale():
+    args = {**dict(host=index().host_ptr, dev=P), **ATTN, "scale": float("inf")}
+    assert gen.lib.harts_gen_attn(*args.values()) == EINVAL

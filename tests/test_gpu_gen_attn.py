@@ -401,3 +401,18 @@ def test_pages_far_into_a_large_cache(kind, rows):
         s = torch.einsum("hgd,thd->hgt", q[r].double().view(hkv, 16, 128), kv[0][:p + 1].double()) * 0.1
         ref = torch.einsum("hgt,thd->hgd", torch.softmax(s, -1), kv[1][:p + 1].double()).reshape(-1, 128)
         assert float((o[r].double() - ref).norm() / ref.norm()) <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,G", [(1, 4), (3, 4), (16, 8), (40, 4)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_of_nan_or_infinity_reaches_no_other(kind, n, G, bad):
+    tree = Tree([0, n + 1], [-1] + [0] * n, [0] + [700] * n, [700] + [70] * n, 32, 2, kind, 5)
+    node, pos = list(range(1, n + 1)), [69] * n
+    index, q = tree.index(node, pos, G), queries(n, 2 * G, 1)
+    o, lse, _ = run(tree, index, q, pos, 0.09)
+    q[n // 2, 1, 5] = bad
+    o2, lse2, _ = run(tree, index, q, pos, 0.09)
+    assert bool(torch.isnan(o2[n // 2, 1]).all()) and not math.isfinite(float(lse2[n // 2, 1]))
+    o2[n // 2, 1], lse2[n // 2, 1] = o[n // 2, 1], lse[n // 2, 1]
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)

@@ -268,3 +268,19 @@ def test_sequences_that_share_rows_beyond_the_workspace_are_refused_on_the_devic
         H.harts_la_check(status)
     assert e.value.code == -1
     assert bool(torch.isnan(o).all()) and not pool.any()
+
+
+@pytest.mark.parametrize("dtype,d,lens", [("bf16", 128, [5, 1]), ("fp32", 128, [9, 100]), ("bf16", 128, [300, 77, 1200])])
+@pytest.mark.parametrize("value,every", [(float("-inf"), 7), (-1e30, 5), (-3000.0, 1), (-100.0, 2)])
+def test_decays_that_leave_nothing(dtype, d, lens, value, every):
+    """A gate of any size, minus infinity too, forgets the state and disturbs no row behind it."""
+    q, k, v, g, states, begin, ins, outs = problem(lens, 2, d, dtype, 3)
+    g[::every] = value
+    ref_o, ref_s = oracle(q, k, v, g, states, begin, lens, ins, outs)
+    o, status = call(q, k, v, g, states, begin, lens, ins, outs)
+    H.harts_la_check(status)
+    ts, to = tol(dtype, dtype == "bf16")
+    assert rel(o, ref_o) <= to
+    for i in outs:
+        if i >= 0:
+            assert rel(states[i], ref_s[i]) <= ts
