@@ -25,6 +25,8 @@ constexpr int PIECE = 2;                // tiles that a unit costs besides its o
 constexpr int64_t SMALL = SMS * 256;
 constexpr int SMALL_ROWS = 32;
 
+constexpr size_t MAX_ENTRIES = (size_t)INT32_MAX / (sizeof(Entry) / 4);        // more do not fit into the index
+
 struct Range {
     int node, a, b, entry, n_entries;
     bool wide;
@@ -37,10 +39,8 @@ struct Index {
 };
 
 bool forest_ok(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const int32_t* off, const int32_t* len) {
-    if (ptr[0] != 0) return false;
     for (int32_t t = 0; t < n_trees; t++) {
         const int32_t lo = ptr[t], hi = ptr[t + 1];
-        if (hi <= lo) return false;
         for (int32_t i = lo; i < hi; i++) {
             if (len[i] < 0) return false;
             if (i == lo ? (parent[i] != -1 || off[i] != 0) : (parent[i] < 0 || parent[i] >= i - lo || off[i] < 0 || off[i] > len[lo + parent[i]])) return false;
@@ -72,9 +72,8 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
     for (int32_t v = 0; v < n_nodes; v++) tokens += sees[v].empty() ? 0 : len[v];
     const int64_t most_rows = tokens * Hkv < SMALL ? SMALL_ROWS : NARROW_ROWS;
     std::vector<Range> ranges;
-    std::vector<int32_t> parts_of(n_q, 0);
     auto add = [&](int node, int a, int b, bool wide, const std::vector<Entry>& e) {
-        if (e.empty() || b <= a) return;
+        if (e.empty() || b <= a || ix.entries.size() >= MAX_ENTRIES) return;
         ranges.push_back({node, a, b, (int)ix.entries.size(), (int)e.size(), wide && (int64_t)e.size() * G > most_rows});
         ix.entries.insert(ix.entries.end(), e.begin(), e.end());
     };
@@ -89,7 +88,7 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
                 least = std::min<int64_t>(least, q_pos[x.row] + 1);
             }
         const int64_t room = ((int64_t)page_ptr[v + 1] - page_ptr[v]) * page, most = std::min<int64_t>((int64_t)len[v] + (n_own ? grow : 0), room);
-        if (room < len[v] || most >= INT32_MAX - TILE) return HARTS_EINVAL;
+        if (room < len[v] || most >= INT32_MAX - (1 << 16)) return HARTS_EINVAL;
         for (int32_t p = page_ptr[v]; p < page_ptr[v + 1]; p++) {
             if (pages[p] < 0) return HARTS_EINVAL;
             ix.max_page = std::max(ix.max_page, pages[p]);
@@ -134,6 +133,7 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
             add(v, own_from, (int)most, false, e);
         }
     }
+    if (ix.entries.size() >= MAX_ENTRIES) return HARTS_EINVAL;
     // Rows of a narrow unit: eight where no run of few rows has more (the kernel is the faster of the two).
     auto tiles_of = [](int a, int b) { return (int64_t)(b + TILE - 1) / TILE - a / TILE; };
     int block_rows = 8;
@@ -284,9 +284,14 @@ extern "C" int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_nod
     if (n_trees < 0 || n_q < 0 || grow < 0 || !tree_node_ptr || !node_page_ptr || !n_words || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 || (int64_t)n_q * Hq > INT32_MAX ||
         (page != 16 && page != 32 && page != 64 && page != 128))
         return HARTS_EINVAL;
-    if (tree_node_ptr[0] != 0 || tree_node_ptr[n_trees] < 0 || node_page_ptr[0] != 0) return HARTS_EINVAL;
-    if (tree_node_ptr[n_trees] > 0 && (!node_parent || !node_fork_off || !node_len)) return HARTS_EINVAL;
+    if (tree_node_ptr[0] != 0 || node_page_ptr[0] != 0) return HARTS_EINVAL;
+    if (n_trees > 0 && (!node_parent || !node_fork_off || !node_len)) return HARTS_EINVAL;
     if (n_q > 0 && (!q_node || !q_pos)) return HARTS_EINVAL;
+    // ascending, before anything is read at their places: what lies between is then inside the arrays
+    for (int32_t t = 0; t < n_trees; t++)
+        if (tree_node_ptr[t + 1] <= tree_node_ptr[t]) return HARTS_EINVAL;
+    for (int32_t v = 0; v < tree_node_ptr[n_trees]; v++)
+        if (node_page_ptr[v + 1] < node_page_ptr[v]) return HARTS_EINVAL;
     try {
         if (!forest_ok(n_trees, tree_node_ptr, node_parent, node_fork_off, node_len)) return HARTS_EINVAL;
         if (node_page_ptr[tree_node_ptr[n_trees]] > 0 && !node_page) return HARTS_EINVAL;

@@ -140,3 +140,11 @@ def test_what_is_refused(bad):
     with pytest.raises(H.HartsError) as e:
         H.harts_gen_attn_index(**{**GOOD, **bad})
     assert e.value.code == -1
+
+
+@pytest.mark.parametrize("bad", [dict(tree_node_ptr=[0, 1 << 28, 2]), dict(tree_node_ptr=[0, -5, 2]), dict(tree_node_ptr=[0, 0, 2]),
+                                 dict(node_page_ptr=[0, 1 << 28, 2]), dict(node_page_ptr=[0, -1, 2]), dict(node_page_ptr=[0, 3, 2])])
+def test_pointers_that_do_not_ascend_are_refused_before_they_are_followed(bad):
+    with pytest.raises(H.HartsError) as e:
+        H.harts_gen_attn_index(**{**GOOD, **bad})
+    assert e.value.code == -1
