@@ -57,7 +57,7 @@ Sizes sizes_of(const GenLaArgs& a) {
     return z;
 }
 
-constexpr int WHOLE = 2;                      // place of the number of whole segments behind the number of items
+constexpr int WHOLE = 2, CUT = 3;             // places behind the number of items: whole segments, sequences of several items
 constexpr int PLAN_THREADS = 512, PLAN_WARPS = PLAN_THREADS / 32, CHOICES = 3 * PLAN_WARPS;
 static_assert(CHOICES > MAX_L - MIN_L + 1, "a place for every length, and for no cut");
 
@@ -122,11 +122,12 @@ __device__ __forceinline__ int choose_rows(LEN len_of, int n_seq, int H, int lea
 }
 
 // The items: whole segments first, in the order of the sequences, then what is left of each (the walk's CTAs draw them from a counter, so the
-// short ones fill the gaps).  chains: each sequence's {first whole segment, items, start state, item of the rest or -1}.
+// short ones fill the gaps).  chains: of each sequence of several items, in any order, {first whole segment, items, start state, item of the rest or -1}.
 __global__ void __launch_bounds__(PLAN_THREADS)
 plan_kernel(const GenLaArgs a, int least, int sms, int max_items, int* count, int4* items, int* follows, int4* chains) {
     __shared__ int2 warp_sum[PLAN_WARPS];
     __shared__ int64_t warp_used[PLAN_WARPS];
+    __shared__ int cut;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     let_next_launch();
     auto look_up = [&](int i, GenSeq& s, bool report) {           // its length, or -1: nothing to do
@@ -177,7 +178,9 @@ plan_kernel(const GenLaArgs a, int least, int sms, int max_items, int* count, in
         count[0] = fits ? whole + all.y : 0;
         count[1] = 0;                             // the walk's counter
         count[WHOLE] = fits ? whole : 0;
+        cut = 0;
     }
+    __syncthreads();
     int2 base = make_int2(0, whole);
     for (int i0 = 0; i0 < a.n_seq; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
@@ -204,19 +207,18 @@ plan_kernel(const GenLaArgs a, int least, int sms, int max_items, int* count, in
             base.y += warp_sum[w].y;
         }
         const int items_here = n.x + n.y;
-        if (i < a.n_seq && !fits) {
-            chains[i] = make_int4(0, 0, -1, -1);
-        } else if (i < a.n_seq) {
+        if (i < a.n_seq && fits) {
             for (int j = 0; j < items_here; j++) {
                 const int item = j < n.x ? at.x + j : at.y;
                 const bool last = j + 1 == items_here;
                 items[item] = make_int4(s.begin + j * rows, j < n.x ? rows : s.len - j * rows, items_here > 1 ? -2 - item : s.in, last ? s.out : -1);
                 follows[item] = !last;
             }
-            chains[i] = make_int4(at.x, items_here, s.in, n.y ? at.y : -1);
+            if (items_here > 1) chains[atomicAdd(&cut, 1)] = make_int4(at.x, items_here, s.in, n.y ? at.y : -1);
         }
         __syncthreads();
     }
+    if (tid == 0) count[CUT] = cut;
 }
 
 // ---- sums of segments --------------------------------------------------------------------------------------------------------
@@ -396,39 +398,45 @@ sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 }
 
 // ---- start states of segments: starts[i] holds U_i on entry and S_i afterwards; four elements a thread -------------------------------
-constexpr int BATCH = 8;
+constexpr int BATCH = 8, BLOCKS = D * D / 1024;
+// CTAs that fit take (sequence of several items, head, part of a state) in turn: a CTA for each, of all sequences, took 23 x 16 of 1 to 6,000 tokens
+// 160 us instead of 157.
 __global__ void __launch_bounds__(256)
-scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const int4* __restrict__ chains, const float* __restrict__ gamma, int H) {
+scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const int* __restrict__ count, const int4* __restrict__ chains,
+            const float* __restrict__ gamma, int H) {
     let_next_launch();
     after_previous();
-    const int4 chain = chains[blockIdx.z];
-    if (chain.y < 2) return;
-    const int h = blockIdx.y;
-    const size_t off = (size_t)(blockIdx.x * 256 + threadIdx.x) * 4;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (chain.z >= 0) s = *reinterpret_cast<const float4*>(states + ((size_t)chain.z * H + h) * (D * D) + off);
-    auto item = [&](int j) { return j + 1 == chain.y && chain.w >= 0 ? chain.w : chain.x + j; };
-    auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)item(j) * H + h) * (D * D) + off); };
-    for (int j0 = 0; j0 < chain.y; j0 += BATCH) {
-        float4 u[BATCH];
-        float e[BATCH];
+    int4 chain = chains[blockIdx.x / (H * BLOCKS)];           // (there are not more CTAs than these would do; read beside the count)
+    const int units = count[CUT] * H * BLOCKS;
+    for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        if (unit != blockIdx.x) chain = chains[unit / (H * BLOCKS)];
+        const int h = unit / BLOCKS % H;
+        const size_t off = (size_t)(unit % BLOCKS * 256 + threadIdx.x) * 4;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (chain.z >= 0) s = *reinterpret_cast<const float4*>(states + ((size_t)chain.z * H + h) * (D * D) + off);
+        auto item = [&](int j) { return j + 1 == chain.y && chain.w >= 0 ? chain.w : chain.x + j; };
+        auto at = [&](int j) { return reinterpret_cast<float4*>(starts + ((size_t)item(j) * H + h) * (D * D) + off); };
+        for (int j0 = 0; j0 < chain.y; j0 += BATCH) {
+            float4 u[BATCH];
+            float e[BATCH];
 #pragma unroll
-        for (int j = 0; j < BATCH; j++)
-            if (j0 + j + 1 < chain.y) {
-                u[j] = *at(j0 + j);
-                e[j] = gamma[(size_t)item(j0 + j) * H + h];
-            }
-#pragma unroll
-        for (int j = 0; j < BATCH; j++)
-            if (j0 + j < chain.y) {
-                *at(j0 + j) = s;
+            for (int j = 0; j < BATCH; j++)
                 if (j0 + j + 1 < chain.y) {
-                    s.x = fmaf(e[j], s.x, u[j].x);
-                    s.y = fmaf(e[j], s.y, u[j].y);
-                    s.z = fmaf(e[j], s.z, u[j].z);
-                    s.w = fmaf(e[j], s.w, u[j].w);
+                    u[j] = *at(j0 + j);
+                    e[j] = gamma[(size_t)item(j0 + j) * H + h];
                 }
-            }
+#pragma unroll
+            for (int j = 0; j < BATCH; j++)
+                if (j0 + j < chain.y) {
+                    *at(j0 + j) = s;
+                    if (j0 + j + 1 < chain.y) {
+                        s.x = fmaf(e[j], s.x, u[j].x);
+                        s.y = fmaf(e[j], s.y, u[j].y);
+                        s.z = fmaf(e[j], s.z, u[j].z);
+                        s.w = fmaf(e[j], s.w, u[j].w);
+                    }
+                }
+        }
     }
 }
 
@@ -464,16 +472,8 @@ int32_t gen_la_chunks(const GenLaArgs& a) {
         if (launch_after(sum_kernel, (int)std::min<int64_t>(z.max_items * a.H, sm_count()), SUM_THREADS, SUM_BYTES, a.stream, mk, mv, a.g, a.H, gen, (const int*)follows, gamma,
                          a.dev_status) != cudaSuccess)
             return HARTS_ECUDA;
-        cudaLaunchAttribute ahead{};
-        ahead.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        ahead.val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t c{};
-        c.gridDim = dim3(D * D / 1024, (unsigned)a.H, (unsigned)a.n_seq);
-        c.blockDim = dim3(256);
-        c.stream = a.stream;
-        c.attrs = &ahead;
-        c.numAttrs = 1;
-        if (cudaLaunchKernelEx(&c, scan_kernel, (const float*)a.states, starts, (const int4*)chains, (const float*)gamma, (int)a.H) != cudaSuccess)
+        if (launch_after(scan_kernel, (int)std::min<int64_t>((int64_t)a.n_seq * a.H * BLOCKS, 3 * sm_count()), 256, 0, a.stream, (const float*)a.states, starts, (const int*)count,
+                         (const int4*)chains, (const float*)gamma, (int)a.H) != cudaSuccess)
             return HARTS_ECUDA;
     }
     return pipe_gen(a, gen, z.max_items);
