@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "gen.h"
@@ -18,6 +19,7 @@ using namespace harts::gen_attn;
 constexpr int TILE = 64;
 constexpr int MIXED = 2 * TILE;         // limits this near to each other share a run
 constexpr int LEAST = 256;              // tokens a wide unit is not cut below
+constexpr int START = 20 * TILE;        // tokens that it counts for besides its own: queries, outputs and the merge of its parts
 constexpr int SMS = 148;
 constexpr int PIECE = 2;                // tiles that a unit costs besides its own, and that are not cut off one
 // Below so many tokens (one short unit an SM, all key heads) a call's time is the kernels' latency, and the narrow kernel's is the shorter:
@@ -172,24 +174,45 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
         return n_parts <= INT32_MAX - (1 << 20);
     };
 
-    // The wide kernel's runs: the shortest pieces that still make one wave; with more units than that anyway, pieces of two thirds of a CTA's
-    // share.
-    int64_t total = 0, units = 0, lo = LEAST, hi = LEAST;
+    // The wide kernel's runs are cut into pieces of at most `lo` tokens, by what a length should take: the longest piece where all of them run at
+    // once, else a CTA's share and a quarter of the longest piece (the long ones go first).  Against the shortest pieces that run at once,
+    // where there are any, and two thirds of a share: agentic trees in bf16, 282 runs of up to 9,000 tokens, 160 -> 71 us; 13 more forests 0 to
+    // 20 % less, three 2 to 4 % more.
+    int64_t total = 0, most = LEAST;
     for (const Range& r : ranges)
         if (r.wide) {
             total += blocks(r, WIDE_ROWS) * (r.b - r.a) * Hkv;
-            units += blocks(r, WIDE_ROWS) * Hkv;
-            hi = std::max<int64_t>(hi, r.b - r.a);
+            most = std::max<int64_t>(most, r.b - r.a);
         }
-    const int64_t want = SMS * (beside ? 1 : 2);
-    if (units > want) lo = hi = std::max<int64_t>(LEAST, 2 * total / (3 * want));
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        int64_t n = 0;
+    const int64_t want = SMS * (beside ? 1 : 2), share = total / want;
+    auto estimate = [&](int64_t p) {
+        int64_t n = 0, longest = 0;
         for (const Range& r : ranges)
-            if (r.wide) n += blocks(r, WIDE_ROWS) * Hkv * ((r.b - r.a + mid - 1) / mid);
-        if (n <= want) hi = mid;
-        else lo = mid + 1;
+            if (r.wide) {
+                const int64_t pieces = (r.b - r.a + p - 1) / p;
+                n += blocks(r, WIDE_ROWS) * Hkv * pieces;
+                longest = std::max<int64_t>(longest, (r.b - r.a + pieces - 1) / pieces);
+            }
+        return std::make_pair(n <= want ? longest + START : (total + START * n) / want + longest / 4, n);
+    };
+    int64_t lo = most, best = total > 0 ? estimate(most).first : 0;
+    auto weigh = [&](int64_t p) {
+        p = std::min(std::max<int64_t>(p, LEAST), most);
+        const int64_t y = estimate(p).first;
+        if (y < best) {
+            best = y;
+            lo = p;
+        }
+    };
+    if (total > 0) {
+        for (int i = 2; i <= 12; i++) weigh(share * i / 6);
+        int64_t l = LEAST, h = most;              // the shortest pieces that run at once
+        while (l < h) {
+            const int64_t mid = (l + h) / 2;
+            if (estimate(mid).second <= want) h = mid;
+            else l = mid + 1;
+        }
+        weigh(l);
     }
     for (const Range& r : ranges) {
         if (!r.wide) continue;
