@@ -21,7 +21,10 @@ constexpr int MIXED = 2 * TILE;         // limits this near to each other share 
 constexpr int LEAST = 256;              // tokens a wide unit is not cut below
 constexpr int START = 20 * TILE;        // tokens that it counts for besides its own: queries, outputs and the merge of its parts
 constexpr int SMS = 148;
-constexpr int PIECE = 2;                // tiles that a unit costs besides its own, and that are not cut off one
+constexpr int PIECE = 2;                // tiles that are not cut off a narrow unit
+// Tiles that a narrow unit costs besides its own: its rows, queries and first page follow each other.  Counted as two, a list of short units took twice
+// as long as the others: 64 sequences of 2,600 tokens with a branch of 16 and two drafts each, 8 bits, 103 us, 60 with five; 30 of 8,000 68 and 52.
+constexpr int UNIT = 5;
 // Below so many tokens (one short unit an SM, all key heads) a call's time is the kernels' latency, and the narrow kernel's is the shorter:
 // 28 rows x 700 tokens 12.4 against 16.4 us.  Above, from 16 rows on the wide one (agentic trees, 32 rows x 900: 92 against 119 us).
 constexpr int64_t SMALL = SMS * 256;
@@ -252,16 +255,16 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
                 for (int e0 = 0; e0 < r.n_entries; e0 += per_block) {
                     const int n = std::min(per_block, r.n_entries - e0);
                     for (int a = r.a; a < r.b;) {
-                        int64_t take = (share - full - PIECE) / chunks;
+                        int64_t take = (share - full - UNIT) / chunks;
                         const int64_t left = tiles_of(a, r.b);
                         if (full > 0 && take < std::min<int64_t>(left, PIECE)) {
                             close();
-                            take = (share - PIECE) / chunks;
+                            take = (share - UNIT) / chunks;
                         }
                         take = std::max<int64_t>(take, 1);
                         const int b = left <= take ? r.b : (int)((a / TILE + take) * TILE);
                         piece(r, e0, n, a, b);
-                        full += chunks * (tiles_of(a, b) + PIECE);
+                        full += chunks * (tiles_of(a, b) + UNIT);
                         a = b;
                     }
                 }
@@ -271,7 +274,7 @@ int32_t build(int32_t n_trees, const int32_t* ptr, const int32_t* parent, const 
         };
         // the smallest share that needs no more lists than there are CTAs
         auto none = [](auto&&...) {};
-        int64_t lo = std::max<int64_t>((tiles + strips * PIECE) / lists, 2 * PIECE), hi = lo;
+        int64_t lo = std::max<int64_t>((tiles + strips * UNIT) / lists, UNIT + PIECE), hi = lo;
         while (fill(hi, none, none) > lists) hi += hi / 4 + 1;
         while (lo < hi) {
             const int64_t mid = (lo + hi) / 2;
