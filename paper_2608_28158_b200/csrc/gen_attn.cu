@@ -232,6 +232,8 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     for (int r = 0; r < NR; r++) mma16816<false>(ks & 1 ? s2[r] : s[r], a, qb[r][ks][0], qb[r][ks][1]);
                 }
             }
+            fence_async_smem();                   // an arrival alone can pass reads that are still on their way, and the next copy then lands under
+            // them: seen beside the wide kernel, whose products keep shared memory busy (1 call in 250)
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.kempty[rk.st]);
             rk.next();
@@ -393,6 +395,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     for (int r = 0; r < NR; r++) mma16816<false>(acc[r][j], va, pb[r][0], pb[r][1]);
                 }
             }
+            fence_async_smem();                   // (as for the keys)
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.vempty[rv.st]);
             rv.next();

@@ -416,3 +416,26 @@ def test_a_query_of_nan_or_infinity_reaches_no_other(kind, n, G, bad):
     assert bool(torch.isnan(o2[n // 2, 1]).all()) and not math.isfinite(float(lse2[n // 2, 1]))
     o2[n // 2, 1], lse2[n // 2, 1] = o[n // 2, 1], lse[n // 2, 1]
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("prefix", [3000, 4000])
+def test_both_kernels_at_once_give_the_same_bits_every_time(kind, prefix):
+    """Runs of many rows and of few in one call, a thousand times: stages are not overwritten under the reads of the one by the copies of the next."""
+    rng = random.Random(150)
+    ln = [prefix] + [rng.randint(1, 300) for _ in range(150)]
+    tree = Tree([0, 151], [-1] + [0] * 150, [0] + [prefix] * 150, ln, 64, 2, kind, 150)
+    node, pos = list(range(1, 151)), [n - 1 for n in ln[1:]]
+    index, q = tree.index(node, pos, 4), queries(150, 8, 150)
+    assert index.n_wide and index.n_narrow
+    first, bad = None, torch.zeros((), dtype=torch.int64, device="cuda")
+    p = torch.tensor(pos, dtype=torch.int32, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty(150, 8, device="cuda")
+    ws = torch.empty(index.workspace_bytes, dtype=torch.uint8, device="cuda")
+    for _ in range(1000):
+        ws.fill_(255)
+        H.harts_gen_attn(index, q, *tree.cache, p, o, lse, 0.09, workspace=ws, k_exp=tree.exp[0], v_exp=tree.exp[1])
+        now = torch.cat([o.float().flatten(), lse.flatten()]).view(torch.int32)
+        first = now if first is None else first
+        bad += (now != first).any()
+    assert int(bad) == 0
