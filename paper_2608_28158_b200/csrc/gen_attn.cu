@@ -495,7 +495,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
 constexpr int MERGE_WARPS = 4;
 template <int W>
 __global__ void __launch_bounds__(MERGE_WARPS * 32)
-merge_kernel(const Tables t, const float* __restrict__ part_o, const float* __restrict__ part_lse, __nv_bfloat16* __restrict__ o, float* __restrict__ lse) {
+merge_kernel(const Tables t, const float* part_o, const float* part_lse, __nv_bfloat16* __restrict__ o, float* __restrict__ lse) {
     __shared__ float4 so[W][32];
     __shared__ float2 stats[W];
     const int64_t out = (int64_t)blockIdx.x * (MERGE_WARPS / W) + (W == 1 ? threadIdx.x >> 5 : 0);

@@ -236,9 +236,10 @@ struct SumMisc {
 constexpr int SUM_REST = STAGES * STAGE, SUM_MISC = SUM_REST + 4 * TILE, SUM_BYTES = SUM_MISC + sizeof(SumMisc) + 1024;
 static_assert(SUM_BYTES <= 227 * 1024, "shared memory");
 
+// (What the kernel ahead writes is not __restrict__ here and below: loads of what never changes could be moved ahead of the wait for it.)
 __global__ void __launch_bounds__(SUM_THREADS, 1)
 sum_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const float* __restrict__ g, int H,
-           const GenItems gen, const int* __restrict__ follows, float* __restrict__ gamma, int* status) {
+           const GenItems gen, const int* follows, float* __restrict__ gamma, int* status) {
     let_next_launch();
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -402,8 +403,7 @@ constexpr int BATCH = 8, BLOCKS = D * D / 1024;
 // CTAs that fit take (sequence of several items, head, part of a state) in turn: a CTA for each, of all sequences, took 23 x 16 of 1 to 6,000 tokens
 // 160 us instead of 157.
 __global__ void __launch_bounds__(256)
-scan_kernel(const float* __restrict__ states, float* __restrict__ starts, const int* __restrict__ count, const int4* __restrict__ chains,
-            const float* __restrict__ gamma, int H) {
+scan_kernel(const float* __restrict__ states, float* starts, const int* count, const int4* chains, const float* gamma, int H) {
     let_next_launch();
     after_previous();
     int4 chain = chains[blockIdx.x / (H * BLOCKS)];           // (there are not more CTAs than these would do; read beside the count)
