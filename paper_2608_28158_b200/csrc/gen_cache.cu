@@ -3,7 +3,7 @@
 // Eight lanes a row of 128: each has 16 values, so that a row is read by eight 32-byte pieces and written as 8-bit values by eight
 // 16-byte ones.  The scale being a power of two, x 2^-e is exact and rounding is that of the significand alone (values far below the
 // row's largest lose bits as subnormals do).  Bound by the traffic, 512 + 258 bytes a (token, head)
-// either way: 16,385 tokens x 8 heads written in 19.1 us (5.3 TB/s), 24,000 x 4 read in 13.1 (5.6), launches of 4 to 5 us apart.
+// either way: 16,385 tokens x 8 heads written in 19.2 us (5.3 TB/s), 24,000 x 4 read in 13.3 (5.6), launches of 4 to 5 us apart.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 

@@ -23,7 +23,7 @@
 // Rows behind an item's end belong to others and may hold anything: a partial chunk's keys and values are zeroed there.
 // 2.2 us a chunk: 1.3 of weighing, then 0.6 of the products, one after the other on the one pair of tiles for the further terms.  Weighing is
 // one function out of line for all warps that do it, since its copies did not fit the instruction cache beside the rest (31,017 tokens x 4
-// heads in 35 segments, whole call: 89 -> 80 us).
+// heads in 35 segments, whole call then: 89 -> 80 us).
 //
 // What bounds it: HBM where chains are many (4,696 chunks x 32 heads 2,946 -> 2,480 us, 98 KB an item: 5.9 TB/s; 2,389 x 16 in chains of
 // up to 293 chunks 1,230 -> 700), else the 1.5 us of a chunk's busiest role (1,047 x 16 in 64 chains, two slices each: scan and chunk
