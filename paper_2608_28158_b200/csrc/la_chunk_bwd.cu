@@ -286,6 +286,7 @@ chunk_bwd_kernel(const harts_la_tables_t tb, int seq_lo, int seq_hi, int H, cons
                 ldmatrix_x4_trans(frag_addr(aK, lane, Lq, t0, ta), fk[ta]);
             }
             g_part *= rd.gamma;
+            fence_async_smem();                   // an arrival alone can pass reads that are still on their way, and the next copies land there
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.bar_qk_read);
             // this thread's four rows: t0 + 2c, +1, t0 + 8 + 2c, +1

@@ -659,6 +659,7 @@ tc_bwd_kernel(const harts_la_tables_t tb, int seq_lo, int n_items, int H, const 
                 ldmatrix_x4_trans(frag_addr(aQ, lane, Lq, t0, ta), fr.q[ta]);
                 ldmatrix_x4_trans(frag_addr(aK, lane, Lq, t0, ta), fr.k[ta]);
             }
+            fence_async_smem();                   // an arrival alone can pass reads that are still on their way, and the next copies land there
             __syncwarp();
             if (lane == 0) mbar_arrive(&m.bar_qk_read);
             // e^{b_n - b_t} of this thread's four rows: t0 + 2c, +1, t0 + 8 + 2c, +1
