@@ -561,7 +561,8 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 it.own_begin = e.x;
                 it.n_replay = it.replay_base = it.req_lo = it.req_hi = it.chunk_base = 0;
                 it.n_virtual = e.y;
-                it.n_chunks = (e.y + BT - 1) / BT;
+                it.n_chunks = max((e.y + BT - 1) / BT, 1);       // a copied state is a chunk of no rows: products look for the next item's chunk ahead of
+                                                                 // this one's sum, and items without any would fill the ring that the others wait for
                 it.init_slot = e.z;
                 it.out = e.w;
             } else if (!GEN && pos < n_items) {

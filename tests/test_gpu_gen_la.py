@@ -284,3 +284,24 @@ def test_decays_that_leave_nothing(dtype, d, lens, value, every):
     for i in outs:
         if i >= 0:
             assert rel(states[i], ref_s[i]) <= ts
+
+
+@pytest.mark.parametrize("lens,heads", [([1, 0, 3] * 230 + [6000, 2, 2500], 1), ([3840], 2), ([7680, 3840, 1920], 4)])
+def test_segments_beside_many_short_sequences_and_without_a_rest(lens, heads):
+    check(lens, heads, 128, "bf16")
+
+
+@pytest.mark.parametrize("lens,heads", [([0] * 300 + [100] + [0] * 300 + [70, 0], 8), ([0] * 90, 64)])
+def test_copies_of_states_in_a_call_of_chunks(lens, heads):
+    """Forks as sequences without tokens, many in a row: their states come out as they went in."""
+    q, k, v, g, states, begin, ins, outs = problem(lens, heads, 128, "bf16", 12, gaps=1)
+    before = states.clone()
+    o, status = call(q, k, v, g, states, begin, lens, ins, outs, max_len=128)
+    H.harts_la_check(status)
+    for n, i, to in zip(lens, ins, outs):
+        if n == 0 and to >= 0:
+            assert torch.equal(states[to], before[i] if i >= 0 else torch.zeros_like(states[to]))
+    own = torch.zeros(q.shape[0], dtype=torch.bool, device="cuda")
+    for b, n in zip(begin, lens):
+        own[b:b + n] = True
+    assert not torch.isnan(o[own]).any() and bool(torch.isnan(o[~own]).all())
