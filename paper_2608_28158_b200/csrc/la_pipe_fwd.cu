@@ -273,8 +273,9 @@ pipe_fwd_kernel(const harts_la_tables_t tb, const GenItems gen, int seq_lo, int 
                 const size_t from = (size_t)init_slot * H + h;
                 const float* src = (GEN ? state_of(init_slot, h) : slots + from * (D * D)) + in_state;
                 if (!GEN && ticket) alive = flag_wait_warp(flags + from * SLICES + slice, 1, status, &m.dead);
-                // a thread's row is 512 bytes from the next one's: whole sectors at a time, where the array allows it
-                if ((reinterpret_cast<uintptr_t>(slots) & 31) == 0) {
+                // a thread's row is 512 bytes from the next one's: whole sectors at a time, where the array that is read allows it (GEN: the pool and the
+                // workspace are aligned to 16 bytes each, and need not agree in the next bit)
+                if ((reinterpret_cast<uintptr_t>(src) & 31) == 0) {
 #pragma unroll
                     for (int e = 0; e < CW / 8; e++)
                         asm volatile("ld.global.v4.b64 {%0, %1, %2, %3}, [%4];"

@@ -305,3 +305,26 @@ def test_copies_of_states_in_a_call_of_chunks(lens, heads):
     for b, n in zip(begin, lens):
         own[b:b + n] = True
     assert not torch.isnan(o[own]).any() and bool(torch.isnan(o[~own]).all())
+
+
+@pytest.mark.parametrize("lens,heads", [([4000], 2), ([1500, 0, 2049, 70], 4), ([40, 3, 129], 3)])
+@pytest.mark.parametrize("pool_off,ws_off", [(0, 16), (16, 0), (16, 16), (0, 48)])
+def test_bases_of_16_bytes_alignment_only(lens, heads, pool_off, ws_off):
+    """Pool and workspace as slices of larger buffers, each 16 bytes past a multiple of 32 or not: the same bits as in buffers of their own."""
+    q, k, v, g, states, begin, ins, outs = problem(lens, heads, 128, "bf16", 13)
+    first, dev = states.clone(), lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    o1, _ = call(q, k, v, g, first, begin, lens, ins, outs)
+
+    def placed(n_bytes, off):
+        buf = torch.full((n_bytes + 512,), 255, dtype=torch.uint8, device="cuda")
+        at = -buf.data_ptr() % 256 + off
+        assert (buf.data_ptr() + at) % 32 == off % 32
+        return buf[at:at + n_bytes]
+
+    pool = placed(states.numel() * 4, pool_off).view(torch.float32).view(states.shape)
+    pool.copy_(states)
+    ws = placed(H.harts_gen_la_workspace_bytes(len(lens), max(lens), q.shape[0], heads, 128, 128, q.dtype), ws_off)
+    o2, status = torch.full_like(o1, float("nan")), torch.zeros(4, dtype=torch.int32, device="cuda")
+    H.harts_gen_la(q, k, v, g, o2, pool, dev(begin), dev(lens), dev(ins), dev(outs), max(lens), workspace=ws, dev_status=status)
+    H.harts_la_check(status)
+    assert torch.equal(o1, o2) and torch.equal(first, pool)
