@@ -72,6 +72,16 @@ __device__ __forceinline__ void widen16(const uint4& y, int exp, uint4* z) {
 #pragma unroll
         for (int i = 0; i < 8; i++) r[i] = times(r[i], e2);
     }
+    // 0x7f and 0xff are NaN, which moving made 480: the only bytes whose lower seven bits carry into the eighth when 1 is added
+    uint32_t nan[4], any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) any |= nan[i] = (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+    if (any & 0x80808080u)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            r[2 * i] |= ((__byte_perm(nan[i], 0, 0x1404) >> 15) & 0x00010001u) * 0x7fffu;
+            r[2 * i + 1] |= ((__byte_perm(nan[i], 0, 0x3424) >> 15) & 0x00010001u) * 0x7fffu;
+        }
     z[0] = make_uint4(r[0], r[1], r[2], r[3]);
     z[1] = make_uint4(r[4], r[5], r[6], r[7]);
 }

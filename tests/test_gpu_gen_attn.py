@@ -439,3 +439,33 @@ def test_both_kernels_at_once_give_the_same_bits_every_time(kind, prefix):
         first = now if first is None else first
         bad += (now != first).any()
     assert int(bad) == 0
+
+
+@pytest.mark.parametrize("branches", [2, 40])
+@pytest.mark.parametrize("place", ["value", "value row", "key", "key row"])
+def test_nan_in_an_8_bit_cache_comes_out_whichever_kernel_reads_it(branches, place):
+    """A byte that is NaN, or a row whose power is, in the prompt that all branches see: read by few rows, and by many (the wide kernel)."""
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, "e4m3", 21)
+    node, pos = list(range(1, branches + 1)), [69] * branches
+    index, q = tree.index(node, pos, 4), queries(branches, 8, 21)
+    assert (index.n_wide > 0) == (branches > 16)
+    want = torch.zeros(branches, 8, 128, dtype=torch.bool, device="cuda")
+    seen = tree.oracle(q, node, pos, 0.1)
+    for token, byte, d in ((5, 0x7f, 3), (333, 0xff, 124), (699, 0x7f, 17)):
+        s = tree.slots[0][token]
+        if place == "value":
+            tree.cache[1].view(torch.uint8)[s // 32, 0, s % 32, d] = byte
+            want[:, :4, d] = True                     # the heads of key head 0
+        elif place == "key":
+            tree.cache[0].view(torch.uint8)[s // 32, 0, s % 32, d] = byte
+        else:
+            tree.exp[place == "value row"][s // 32, 0, s % 32] = 255
+        if place != "value":
+            want[:, :4] = True
+    o, lse, status = run(tree, index, q, pos, 0.1)
+    H.harts_la_check(status)
+    assert torch.equal(torch.isnan(o), want)
+    assert torch.equal(torch.isnan(lse), want.all(-1) & place.startswith("key"))
+    rest = ~want
+    d = (o.double() - seen[0])[rest]
+    assert float(d.norm() / seen[0][rest].norm()) <= 2.0 ** -8
