@@ -621,8 +621,13 @@ int32_t gen_attn_launch(const int32_t* hi, const int32_t* di, const void* q, int
     if (hi[MERGED]) {
         const int heads = t.n_q * t.Hq;           // (it fits: the index saw to it)
         const bool few = heads <= 4 * sm_count();
-        if (launch_after(few ? merge_kernel<4> : merge_kernel<1>, few ? heads : (int)(((int64_t)heads + MERGE_WARPS - 1) / MERGE_WARPS), MERGE_WARPS * 32, 0, st, t,
-                         (const float*)part_o, (const float*)part_lse, (__nv_bfloat16*)o, lse) != cudaSuccess)
+        auto* kernel = few ? merge_kernel<4> : merge_kernel<1>;
+        const int grid = few ? heads : (int)(((int64_t)heads + MERGE_WARPS - 1) / MERGE_WARPS);
+        if (hi[N_NARROW] == 0 && hi[N_WIDE] == 0) {           // nobody sees anything: this is the call's first kernel, and what ran before may have written the index
+            kernel<<<grid, MERGE_WARPS * 32, 0, st>>>(t, part_o, part_lse, static_cast<__nv_bfloat16*>(o), lse);
+            return cudaGetLastError() == cudaSuccess ? HARTS_OK : HARTS_ECUDA;
+        }
+        if (launch_after(kernel, grid, MERGE_WARPS * 32, 0, st, t, (const float*)part_o, (const float*)part_lse, (__nv_bfloat16*)o, lse) != cudaSuccess)
             return HARTS_ECUDA;
     }
     return HARTS_OK;

@@ -1,4 +1,5 @@
 """harts_gen_attn on the GPU: attention of sampled tokens on a cached tree against its definition, query by query in 64 bits."""
+import ctypes
 import math
 import random
 
@@ -469,3 +470,44 @@ def test_nan_in_an_8_bit_cache_comes_out_whichever_kernel_reads_it(branches, pla
     rest = ~want
     d = (o.double() - seen[0])[rest]
     assert float(d.norm() / seen[0][rest].norm()) <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("node,q_pos", [([1, 1], [-1, -1]), ([0, 1], [299, 9])])
+def test_a_call_s_first_kernel_waits_for_what_ran_before(node, q_pos):
+    """What fills the index on the device may be the kernel right before the call: no kernel of the call is launched ahead of it, also where
+    there is nothing to see and the merge is the only one.  (Of a captured call: edges of type 1 let a kernel start before the one ahead is complete.)"""
+    tree = Tree([0, 2], [-1, 0], [0, 0 if q_pos[0] < 0 else 300], [300, q_pos[1] + 1], 32, 2, "bf16", 22)
+    index, q = tree.index(node, q_pos, 4), queries(2, 8, 22)
+    assert (index.n_narrow + index.n_wide > 0) == (q_pos[0] >= 0)
+    o, lse, pos = torch.empty_like(q), torch.empty(2, 8, device="cuda"), torch.tensor(q_pos, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(16, index.workspace_bytes), dtype=torch.uint8, device="cuda")
+    blob = index.dev.clone()
+
+    def work():
+        index.dev.copy_(blob + 0)                     # a kernel, then a copy
+        index.dev.add_(0)                             # and a kernel right before the call
+        H.harts_gen_attn(index, q, *tree.cache, pos, o, lse, 0.1, workspace=ws)
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        work()
+    driver, n = ctypes.CDLL("libcuda.so.1"), ctypes.c_size_t(0)
+    raw = ctypes.c_void_p(graph.raw_cuda_graph())
+    assert driver.cuGraphGetEdges_v2(raw, None, None, None, ctypes.byref(n)) == 0
+    start, end, kind = (ctypes.c_void_p * n.value)(), (ctypes.c_void_p * n.value)(), (ctypes.c_uint8 * (8 * n.value))()
+    assert driver.cuGraphGetEdges_v2(raw, start, end, kind, ctypes.byref(n)) == 0
+    after = {a: (b, kind[8 * i + 2]) for i, (a, b) in enumerate(zip(start, end))}       # a chain; an edge's bytes are from, to, type
+    at, ahead = next(a for a in start if a not in set(end)), []
+    while at in after:
+        at, k = after[at]
+        ahead.append(k)
+    assert len(ahead) == n.value
+    # sum, copy, sum, the call's first kernel; a merge behind it is launched ahead of its end
+    assert ahead == [0, 0, 0] + [1] * (q_pos[0] >= 0)
+    graph.instantiate()
+    o.fill_(float("nan"))
+    graph.replay()
+    torch.cuda.synchronize()
+    compare(o, lse, *tree.oracle(q, node, q_pos, 0.1))
