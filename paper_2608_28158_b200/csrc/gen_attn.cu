@@ -240,7 +240,10 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
 #pragma unroll
             for (int r = 0; r < NR; r++)
 #pragma unroll
-                for (int x = 0; x < 4; x++) s[r][x] = (s[r][x] + s2[r][x]) * (F8 ? f[r][x & 1] * kp[x >> 1] : f[r][x & 1]);
+                for (int x = 0; x < 4; x++) {          // (8 bits: the two factors' product may be beyond fp32 where a score is not)
+                    s[r][x] = (s[r][x] + s2[r][x]) * f[r][x & 1];
+                    if constexpr (F8) s[r][x] *= kp[x >> 1];
+                }
         };
         constexpr bool EARLY = NR == 1;           // (the registers of 16 rows do not allow it)
         float s[NR][4], ahead[EARLY ? NR : 1][4];

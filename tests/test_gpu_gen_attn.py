@@ -511,3 +511,19 @@ def test_a_call_s_first_kernel_waits_for_what_ran_before(node, q_pos):
     graph.replay()
     torch.cuda.synchronize()
     compare(o, lse, *tree.oracle(q, node, q_pos, 0.1))
+
+
+@pytest.mark.parametrize("branches", [2, 40])
+def test_large_queries_and_large_keys_that_are_orthogonal(branches):
+    """All scores are 0, whatever the factors: the values' mean."""
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, "e4m3", 24)
+    tree.cache[0].view(torch.uint8)[..., 5] = 0
+    tree.exp[0].fill_(247)
+    tree.values[0] = tree.cache[0].float().double() * 2.0 ** 120
+    node, pos = list(range(1, branches + 1)), [69] * branches
+    index, q = tree.index(node, pos, 4), torch.zeros(branches, 8, 128, dtype=torch.bfloat16, device="cuda")
+    q[..., 5] = 2.0 ** 40
+    assert (index.n_wide > 0) == (branches > 16)
+    o, lse, status = run(tree, index, q, pos, 0.1)
+    H.harts_la_check(status)
+    compare(o, lse, *tree.oracle(q, node, pos, 0.1))
