@@ -187,13 +187,14 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 limit[r][y] = __shfl_sync(~0u, mine.limit, 8 * r + 2 * c + y);         // (0 behind the unit's rows)
             }
         }
-        // top: of a score; top2: of a score and its value's power (8 bits), which p goes by
-        float acc[NR][8][4], top[NR][2], top2[NR][2], sum[NR][2];
+        // top: of a score.  8 bits: what p goes by is top + ahead, the largest of a score and its value's power; `ahead` for itself, as the sum would
+        // round the power off beside a large score.
+        float acc[NR][8][4], top[NR][2], ahead[NR][2], sum[NR][2];
 #pragma unroll
         for (int r = 0; r < NR; r++) {
 #pragma unroll
             for (int j = 0; j < 8; j++) acc[r][j][0] = acc[r][j][1] = acc[r][j][2] = acc[r][j][3] = 0.f;
-            top[r][0] = top[r][1] = top2[r][0] = top2[r][1] = -INFINITY;
+            top[r][0] = top[r][1] = ahead[r][0] = ahead[r][1] = -INFINITY;
             sum[r][0] = sum[r][1] = 0.f;
         }
         // scores of a tile's tokens 16 warp + g and + 8, in log2 units
@@ -246,15 +247,15 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 }
         };
         constexpr bool EARLY = NR == 1;           // (the registers of 16 rows do not allow it)
-        float s[NR][4], ahead[EARLY ? NR : 1][4];
+        float s[NR][4], next[EARLY ? NR : 1][4];
         if constexpr (EARLY)
-            if (n_tiles > 0) scores(ahead);
+            if (n_tiles > 0) scores(next);
         for (int n = 0; n < n_tiles && alive; n++) {
             const int j0 = tile0 + n * TILE, key0 = j0 + 16 * warp;
             if constexpr (EARLY) {                // the next tile's products run under this one's softmax
 #pragma unroll
-                for (int x = 0; x < 4; x++) s[0][x] = ahead[0][x];
-                if (n + 1 < n_tiles) scores(ahead);
+                for (int x = 0; x < 4; x++) s[0][x] = next[0][x];
+                if (n + 1 < n_tiles) scores(next);
             } else {
                 scores(s);
             }
@@ -279,35 +280,38 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                     }
             // maxima are looked for only where some score is 2^8 above what its row goes by (or has nothing to go by yet)
             bool over = false;
+            auto from = [&](float m) { return m == -INFINITY ? 0.f : m; };         // what is measured from a maximum: of nothing yet, from 0
 #pragma unroll
             for (int r = 0; r < NR; r++)
 #pragma unroll
                 for (int x = 0; x < 4; x++) {
                     over |= s[r][x] > top[r][x & 1] + RAISE;
-                    if constexpr (F8) over |= s[r][x] + ve[x >> 1] > top2[r][x & 1] + RAISE;
+                    if constexpr (F8) over |= s[r][x] - from(top[r][x & 1]) + ve[x >> 1] > ahead[r][x & 1] + RAISE;
                 }
             if (__any_sync(~0u, over)) {
 #pragma unroll
                 for (int r = 0; r < NR; r++)
 #pragma unroll
                     for (int y = 0; y < 2; y++) {
-                        float mx = fmaxf(s[r][y], s[r][2 + y]), mx2 = F8 ? fmaxf(s[r][y] + ve[0], s[r][2 + y] + ve[1]) : 0.f;
+                        float mx = fmaxf(s[r][y], s[r][2 + y]);
 #pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) {
-                            mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
-                            if constexpr (F8) mx2 = fmaxf(mx2, __shfl_xor_sync(~0u, mx2, x));
-                        }
+                        for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
                         float by = 1.f;           // (from -inf: 0, and all sums are 0)
                         if (mx > top[r][y] + RAISE) {
                             by = ex2(top[r][y] - mx);
                             sum[r][y] *= by;
+                            ahead[r][y] += from(top[r][y]) - mx;
                             top[r][y] = mx;
                         }
                         if constexpr (F8) {
+                            const float base = from(top[r][y]);
+                            float mx2 = fmaxf(s[r][y] - base + ve[0], s[r][2 + y] - base + ve[1]);
+#pragma unroll
+                            for (int x = 4; x < 32; x <<= 1) mx2 = fmaxf(mx2, __shfl_xor_sync(~0u, mx2, x));
                             by = 1.f;
-                            if (mx2 > top2[r][y] + RAISE) {
-                                by = ex2(top2[r][y] - mx2);
-                                top2[r][y] = mx2;
+                            if (mx2 > ahead[r][y] + RAISE) {
+                                by = ex2(ahead[r][y] - mx2);
+                                ahead[r][y] = mx2;
                             }
                         }
 #pragma unroll
@@ -323,12 +327,13 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                 float p[4];
 #pragma unroll
                 for (int y = 0; y < 2; y++) {
-                    const float base = top[r][y] == -INFINITY ? 0.f : top[r][y], base2 = top2[r][y] == -INFINITY ? 0.f : top2[r][y];
+                    const float base = from(top[r][y]), base2 = from(ahead[r][y]);
 #pragma unroll
                     for (int x = y; x < 4; x += 2) {
-                        p[x] = ex2(s[r][x] - base);
+                        const float t = s[r][x] - base;
+                        p[x] = ex2(t);
                         sum[r][y] += p[x];
-                        if constexpr (F8) p[x] = s[r][x] == -INFINITY ? 0.f : ex2(s[r][x] + ve[x >> 1] - base2);      // (a hidden token's power may be anything)
+                        if constexpr (F8) p[x] = t == -INFINITY ? 0.f : ex2(t + (ve[x >> 1] - base2));      // (a hidden token's power may be anything)
                     }
                 }
 #pragma unroll
@@ -405,7 +410,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
         }
         // ---- the four warps' parts joined -----------------------------------------------------------------------------------------
         float* so = reinterpret_cast<float*>(smem + S::joint);
-        float4* stats = reinterpret_cast<float4*>(smem + S::stats);        // [warp][row]{maximum, sum, what outputs go by, -}
+        float4* stats = reinterpret_cast<float4*>(smem + S::stats);        // [warp][row]{maximum, sum, 8 bits: what outputs go by, from the maximum, -}
         constexpr int PER = CW * 4;                                       // threads a row
 #pragma unroll
         for (int r8 = 0; r8 < NR; r8++)
@@ -413,7 +418,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             for (int y = 0; y < 2; y++) {
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) sum[r8][y] += __shfl_xor_sync(~0u, sum[r8][y], x);
-                if (g == 0) stats[warp * ROWS + 8 * r8 + 2 * c + y] = make_float4(top[r8][y], sum[r8][y], F8 ? top2[r8][y] : top[r8][y], 0.f);
+                if (g == 0) stats[warp * ROWS + 8 * r8 + 2 * c + y] = make_float4(top[r8][y], sum[r8][y], F8 ? ahead[r8][y] : top[r8][y], 0.f);
             }
 #pragma unroll
         for (int r8 = 0; r8 < NR; r8++) {
@@ -450,8 +455,8 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
                         for (int x = 0; x < CW; x++) {
                             const float4 y = stats[x * ROWS + i];
                             L += y.x == -INFINITY ? 0.f * y.y : ex2(y.x - M) * y.y;
-                            // a warp's output is in units of 2^top2; without a number there, though it has seen something: NaN
-                            w[x] = y.y == 0.f ? 0.f : y.z == -INFINITY ? __uint_as_float(0x7fffffffu) : ex2(y.z - M);
+                            // without a maximum, though the warp has seen something: NaN
+                            w[x] = y.y == 0.f ? 0.f : y.z == -INFINITY ? __uint_as_float(0x7fffffffu) : ex2(F8 ? y.x - M + y.z : y.x - M);
                         }
                         none = M == -INFINITY && L == 0.f;
                         inv = none ? 0.f : 1.f / L;

@@ -527,3 +527,13 @@ def test_large_queries_and_large_keys_that_are_orthogonal(branches):
     o, lse, status = run(tree, index, q, pos, 0.1)
     H.harts_la_check(status)
     compare(o, lse, *tree.oracle(q, node, pos, 0.1))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches", [2])
+@pytest.mark.parametrize("q_scale", [2.0 ** 16, 2.0 ** 24, 2.0 ** 40, 2.0 ** 90])
+def test_scores_of_any_size(kind, branches, q_scale):
+    """Finite scores of 2^17 to 2^100, of which the largest takes all: its value, to its own rounding."""
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 25)
+    index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 25, q_scale=q_scale)
+    assert (index.n_wide > 0) == (branches > 16)
