@@ -40,7 +40,7 @@ struct Misc {
     uint64_t q, k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, kp_full[2];      // 8 bits: k, kfree are those of the stages of pages
     int dead;
     uint32_t tmem;
-    alignas(16) float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: powers of a tile's keys, and what makes a row's score log2 units
+    alignas(16) float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: factors of a tile's keys and of the rows, which make a sum of products a score in log2 units
 };
 static_assert(offsetof(Misc, kp) <= 256 && offsetof(Misc, kp) % 16 == 0 && sizeof(Misc) <= 1280 && Shape<true>::misc % 16 == 0, "misc area");
 
@@ -92,6 +92,11 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t
 }
 // e4m3 inputs, fp32 sums, both K-major
 __host__ __device__ constexpr uint32_t instr_desc_f8(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+
+// A scale as a power of two and what is left of it, in [1, 2) (below 1 for a subnormal scale).  With a power of two alone, y f - (max y) f is exact whatever the size of the scores; of a
+// product with any factor, a multiply-add would see what rounding took from the maximum: 16 at 2^28, beyond exp2's range at 2^32.
+__device__ __forceinline__ float power_of(float x) { return __uint_as_float(max(__float_as_uint(x) & 0x7f800000u, 0x00800000u)); }
+constexpr float FAR = 268435456.f;       // 2^28
 
 template <bool F8>
 __global__ void __launch_bounds__(Shape<F8>::NT, Shape<F8>::CTAS)
@@ -162,7 +167,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
                 unsigned char* dst = smem + S::q + sw128_chunk(i, ch >> 1) + 8 * (ch & 1);
                 *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
                 *reinterpret_cast<uint2*>(dst + S::Q_BYTES / 2) = make_uint2(lo[0], lo[1]);
-                if (ch == 0) m.f[i] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : f.undone(scale_log2);      // infinite or NaN: NaN
+                if (ch == 0) m.f[i] = top >= 0x7f80u ? __uint_as_float(0x7fffffffu) : f.undone(power_of(scale_log2));      // infinite or NaN: NaN
             } else {
                 *reinterpret_cast<uint4*>(smem + S::q + (ch >> 3) * (S::Q_BYTES / 2) + sw128_chunk(i, ch & 7)) = x;
             }
@@ -276,6 +281,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         // ---- 8-bit pages -> tiles ---------------------------------------------------------------------------------------------------------
         // a quarter of a warp stores to eight different places of two keys' rows of 128 bytes
         const int wt = tid - NS - 64, ch0 = wt & 3, key0 = wt >> 2;
+        const float rest_of_scale = scale_log2 / power_of(scale_log2);
         for (int n = 0; n < n_tiles; n++) {
             const int st = n & 1, j0 = tile0 + n * TILE;
             if (!mbar_wait_warp(&m.k[st], (n >> 1) & 1, status, &m.dead)) break;
@@ -283,7 +289,7 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             if (!mbar_wait_warp(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
             const unsigned char *raw = smem + S::raw + st * S::RAW + TILE * D, *exps = smem + S::raw_exp + st * S::RAW_EXP;
             if (wt < TILE) {
-                m.kp[st][wt] = gen_power(exps[wt]);
+                m.kp[st][wt] = gen_power(exps[wt]) * rest_of_scale;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.kp_full[st]);
             }
@@ -310,9 +316,9 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         // ---- softmax: a row per thread -----------------------------------------------------------------------------------------------------
         const uint32_t tm_lane = tmem + ((uint32_t)(warp * 32) << 16);
         if (F8) mbar_wait_warp(&m.q, 0, status, &m.dead);         // (the rows' factors are other warps')
-        const float scale = F8 ? m.f[tid] : scale_log2;
-        const F2 scale2 = f2(scale, scale);
-        float m_ref = -INFINITY, l_sum = 0.f;
+        // m_ref: the maximum that p goes by.  bf16: scores of FAR and more differ by 16 at least, so the power of the scale is enough of it to tell the
+        // largest; sc and neg_m are what p is made with.
+        float m_ref = -INFINITY, l_sum = 0.f, sc = F8 ? m.f[tid] : scale_log2, neg_m = 0.f;
         for (int n = 0; n < n_tiles; n++) {
             const int b = n & 1, j0 = tile0 + n * TILE;
             if (!mbar_wait_warp(&m.s[b], (n >> 1) & 1, status, &m.dead)) break;
@@ -347,30 +353,33 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
             }
-            mx *= scale;
-            const bool raise = mx > m_ref + RAISE || (m_ref == -INFINITY && mx > -INFINITY);
-            if (__any_sync(~0u, raise && n > 0)) {
-                // O is about to be read and rewritten: the P V MMAs of the tile before must be done (this warp is never more than a phase behind)
-                if (!mbar_wait_warp(&m.pv, (n - 1) & 1, status, &m.dead)) break;
-                tc_fence_after();
-                const float m_new = raise ? mx : m_ref;
-                const float alpha = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
-                l_sum *= alpha;
+            const float top = mx * sc, by = m_ref == -INFINITY ? -INFINITY : -neg_m;
+            const bool raise = top > by + RAISE || (m_ref == -INFINITY && top > -INFINITY);
+            if (__any_sync(~0u, raise)) {
+                const float m_new = raise ? F8 ? top : mx * scale_log2 : m_ref;
+                if (n > 0) {
+                    // O is about to be read and rewritten: the P V MMAs of the tile before must be done (this warp is never more than a phase behind)
+                    if (!mbar_wait_warp(&m.pv, (n - 1) & 1, status, &m.dead)) break;
+                    tc_fence_after();
+                    const float alpha = m_new == -INFINITY ? 1.f : ex2(m_ref - m_new);
+                    l_sum *= alpha;
 #pragma unroll 1
-                for (int c = 0; c < 8; c++) {
-                    uint32_t y[16];
-                    tmem_ld16(tm_lane + COL_O + c * 16, y);
-                    tmem_ld_wait();
+                    for (int c = 0; c < 8; c++) {
+                        uint32_t y[16];
+                        tmem_ld16(tm_lane + COL_O + c * 16, y);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 16; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
-                    tmem_st16(tm_lane + COL_O + c * 16, y);
+                        for (int e = 0; e < 16; e++) y[e] = __float_as_uint(__uint_as_float(y[e]) * alpha);
+                        tmem_st16(tm_lane + COL_O + c * 16, y);
+                    }
                 }
-                m_ref = m_new;
-            } else if (raise) {
-                m_ref = mx;                               // first tile: nothing accumulated yet
+                if (raise) {
+                    m_ref = m_new;
+                    if constexpr (!F8) sc = fabsf(m_ref) >= FAR && fabsf(m_ref) < INFINITY ? power_of(scale_log2) : scale_log2;
+                    neg_m = F8 ? -m_ref : -(mx * sc);
+                }
             }
-            const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;
-            const F2 nm = f2(neg_m, neg_m);
+            const F2 nm = f2(neg_m, neg_m), scale2 = f2(sc, sc);
             F2 part[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
 #pragma unroll
             for (int c = 0; c < 2; c++) {

@@ -530,10 +530,18 @@ def test_large_queries_and_large_keys_that_are_orthogonal(branches):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("branches", [2])
+@pytest.mark.parametrize("branches", [2, 40])
 @pytest.mark.parametrize("q_scale", [2.0 ** 16, 2.0 ** 24, 2.0 ** 40, 2.0 ** 90])
 def test_scores_of_any_size(kind, branches, q_scale):
     """Finite scores of 2^17 to 2^100, of which the largest takes all: its value, to its own rounding."""
     tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 25)
     index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 25, q_scale=q_scale)
     assert (index.n_wide > 0) == (branches > 16)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches", [2, 40])
+@pytest.mark.parametrize("q_scale,scale", [(2.0 ** 110, 2.0 ** -112), (2.0 ** 120, 2.0 ** -127 * 1.5), (2.0 ** -100, 2.0 ** 100), (1.0, 2.0 ** -140)])
+def test_scales_of_any_size(kind, branches, q_scale, scale):
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 26)
+    check(tree, list(range(1, branches + 1)), [69] * branches, 4, 26, q_scale=q_scale, scale=scale)
