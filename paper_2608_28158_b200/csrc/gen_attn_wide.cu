@@ -35,11 +35,16 @@ struct Shape {
     static constexpr int q = 0, k = Q_BYTES, v = k + KB, raw = v + 2 * KV_BYTES, raw_exp = raw + RAWS * RAW, misc = raw_exp + RAWS * RAW_EXP;
     static constexpr int bytes = misc + (F8 ? 1280 : 256) + 1024;
 };
+// The exponent byte from which a key's factor, 2^(byte - 127) to twice that, may take a sum of products beyond fp32: those are below 2^24 (256 x 448 x 128,
+// and the second terms)
+constexpr int LARGE = 127 + 103;
+constexpr float UP = 4294967296.f;       // then 2^32 of it goes with the rows' factors: theirs are small, or the scores would not be finite
 constexpr int COL_S = 0, COL_O = 128, TMEM_COLS = 256;     // S / P of tile n at COL_S + 64 (n & 1)
 struct Misc {
     uint64_t q, k[2], v[2], kfree[2], vfree[2], s[2], p[2], pv, o, exit, kp_full[2];      // 8 bits: k, kfree are those of the stages of pages
     int dead;
     uint32_t tmem;
+    float up[2];                                     // 8 bits: what the rows' factors take from those of a tile's keys
     alignas(16) float kp[2][TILE], f[WIDE_ROWS];     // 8 bits: factors of a tile's keys and of the rows, which make a sum of products a score in log2 units
 };
 static_assert(offsetof(Misc, kp) <= 256 && offsetof(Misc, kp) % 16 == 0 && sizeof(Misc) <= 1280 && Shape<true>::misc % 16 == 0, "misc area");
@@ -289,7 +294,9 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
             if (!mbar_wait_warp(&m.vfree[st], ((n >> 1) & 1) ^ 1, status, &m.dead)) break;
             const unsigned char *raw = smem + S::raw + st * S::RAW + TILE * D, *exps = smem + S::raw_exp + st * S::RAW_EXP;
             if (wt < TILE) {
-                m.kp[st][wt] = gen_power(exps[wt]) * rest_of_scale;
+                const bool large = __any_sync(~0u, max(exps[lane], exps[32 + lane]) >= LARGE);        // (both warps see all keys)
+                m.kp[st][wt] = gen_power(exps[wt]) * (large ? rest_of_scale / UP : rest_of_scale);
+                if (wt == 0) m.up[st] = large ? UP : 1.f;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&m.kp_full[st]);
             }
@@ -318,13 +325,14 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
         if (F8) mbar_wait_warp(&m.q, 0, status, &m.dead);         // (the rows' factors are other warps')
         // m_ref: the maximum that p goes by.  bf16: scores of FAR and more differ by 16 at least, so the power of the scale is enough of it to tell the
         // largest; sc and neg_m are what p is made with.
-        float m_ref = -INFINITY, l_sum = 0.f, sc = F8 ? m.f[tid] : scale_log2, neg_m = 0.f;
+        float m_ref = -INFINITY, l_sum = 0.f, sc = scale_log2, neg_m = 0.f;
         for (int n = 0; n < n_tiles; n++) {
             const int b = n & 1, j0 = tile0 + n * TILE;
             if (!mbar_wait_warp(&m.s[b], (n >> 1) & 1, status, &m.dead)) break;
             if (F8 && !mbar_wait_warp(&m.kp_full[b], (n >> 1) & 1, status, &m.dead)) break;
             tc_fence_after();
             const bool edge = j0 < u.k0 || j0 + TILE > u.k1;
+            if constexpr (F8) sc = m.f[tid] * m.up[b];
             float mx = -INFINITY;
             uint32_t x[32];                           // half a row of S at a time, so that two CTAs' registers fit
             auto half = [&](int c) {

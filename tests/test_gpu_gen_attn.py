@@ -545,3 +545,15 @@ def test_scores_of_any_size(kind, branches, q_scale):
 def test_scales_of_any_size(kind, branches, q_scale, scale):
     tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 26)
     check(tree, list(range(1, branches + 1)), [69] * branches, 4, 26, q_scale=q_scale, scale=scale)
+
+
+# Finite keys of any size against queries that make finite scores of them: both kernels, to the tolerances of every other size.
+@pytest.mark.parametrize("branches", [2, 40])
+@pytest.mark.parametrize("q_scale,lo,hi", [(2.0 ** -113, 228, 237), (2.0 ** -60, 120, 248), (2.0 ** -20, 244, 248), (2.0 ** 60, 1, 60), (2.0 ** 100, 1, 20)])
+def test_keys_of_any_size_in_an_8_bit_cache(branches, q_scale, lo, hi):
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, "e4m3", 23)
+    e = torch.randint(lo, hi, tree.exp[0].shape, device="cuda").to(torch.uint8)
+    tree.exp[0].copy_(e)
+    tree.values[0] = tree.cache[0].float().double() * (e.cpu().double() - 127).exp2().cuda()[..., None]
+    index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 23, q_scale=q_scale)
+    assert (index.n_wide > 0) == (branches > 16)
