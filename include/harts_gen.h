@@ -110,7 +110,7 @@ int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache
  * harts_gen_attn_workspace_bytes: of the parts of split sums.  Calls that share a workspace must not run at the same time.
  * harts_gen_attn: q bf16 [n_q, Hq, 128], heads contiguous, ld_q elements between rows; q_pos device int32 [n_q]; o bf16, lse fp32,
  *   contiguous, written for every query, neither overlapping an input.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
- *   scale is positive and finite.  Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
+ *   scale is positive and at most FLT_MAX ln 2 (2.3e38).  Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
  */
 #define HARTS_GEN_ATTN_HEADER_WORDS 32
 int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_node_ptr, const int32_t* node_parent, const int32_t* node_fork_off,

@@ -136,7 +136,8 @@ int32_t harts_gen_attn(const int32_t* host_index, const int32_t* dev_index, cons
                        int32_t* dev_status, void* stream) {
     using namespace harts::gen_attn;
     size_t need = 0;
-    if (harts_gen_attn_workspace_bytes(host_index, &need) != HARTS_OK || !dev_index || !aligned16(dev_index) || !(scale > 0.f && scale <= FLT_MAX)) return HARTS_EINVAL;
+    constexpr float MOST_SCALE = (float)(FLT_MAX * 0.6931471805599453);            // exponents are base 2: scale / ln 2 has to be a number too
+    if (harts_gen_attn_workspace_bytes(host_index, &need) != HARTS_OK || !dev_index || !aligned16(dev_index) || !(scale > 0.f && scale <= MOST_SCALE)) return HARTS_EINVAL;
     const int32_t rc = cache_check(host_index[N_Q], n_pages, host_index[PAGE], host_index[HKV], 128, cache_type);
     if (rc != HARTS_OK) return rc;
     if (host_index[N_Q] == 0) return HARTS_OK;

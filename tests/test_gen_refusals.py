@@ -141,3 +141,10 @@ def test_tensors_of_the_host_are_refused():
 def test_attn_refuses_an_infinite_scale():
     args = {**dict(host=index().host_ptr, dev=P), **ATTN, "scale": float("inf")}
     assert gen.lib.harts_gen_attn(*args.values()) == EINVAL
+
+
+@pytest.mark.parametrize("scale,code", [(np.finfo(np.float32).max, EINVAL), (2.36e38, EINVAL), (2.3586e38, OK)])
+def test_attn_refuses_a_scale_that_base_2_exponents_cannot_hold(scale, code):
+    """scale / ln 2 in fp32; the one below it is taken (of a call without queries, which launches nothing)."""
+    ix = index() if code else index(q_node=[], q_pos=[])
+    assert gen.lib.harts_gen_attn(*{**dict(host=ix.host_ptr, dev=P), **ATTN, "scale": float(scale)}.values()) == code
