@@ -51,6 +51,23 @@ def _code(where, dtype):
     return _DTYPE_CODE[dtype]
 
 
+def _int32(where, **sizes):
+    """Sizes that the C ABI takes in 32 bits (ctypes would cut them off without a word)."""
+    for name, x in sizes.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            _bad(where, f"{name}: {x} is not a number of 32 bits")
+
+
+def _int32_array(where, name, a):
+    """One-dimensional whole numbers of any type as int32, none of them changed."""
+    a = np.asarray(a)
+    if a.ndim != 1:
+        _bad(where, f"{name}: {a.ndim} dimensions, wants one")
+    if a.dtype != np.int32 and a.size and not (-2 ** 31 <= a.min() <= a.max() < 2 ** 31 and (a.dtype.kind in "iub" or (a == np.rint(a)).all())):
+        _bad(where, f"{name}: numbers from {a.min()} to {a.max()}, wants whole ones of 32 bits")
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
 def _device(where, name, t):
     dev = t.get_device()
     if dev < 0:
@@ -105,6 +122,7 @@ def _call(where, f, dev, stream, *args):
 
 
 def harts_gen_la_workspace_bytes(n_seq, max_len, n_rows, H, dk, dv, dtype) -> int:
+    _int32("harts_gen_la_workspace_bytes", n_seq=n_seq, max_len=max_len, H=H, dk=dk, dv=dv)
     n = _sz(0)
     _check(lib.harts_gen_la_workspace_bytes(n_seq, max_len, n_rows, H, dk, dv, _code("harts_gen_la_workspace_bytes", dtype), C.byref(n)),
            "harts_gen_la_workspace_bytes")
@@ -127,6 +145,8 @@ def harts_gen_la(q, k, v, g, o, states, seq_begin, seq_len, in_state, out_state,
             _bad(w, "o without q")
         ld_q = _rows(w, "q", q, shape, dt, dev)
         o_ptr = _plain(w, "o", o, dt, shape, dev)
+    if not -2 ** 31 <= max_len < 2 ** 31:
+        _int32(w, max_len=max_len)
     i32, one = torch.int32, (n_seq,)
     ws, ws_bytes = _bytes(w, "workspace", workspace, dev)
     _call(w, lib.harts_gen_la, dev, stream, n_seq, _plain(w, "seq_begin", seq_begin, i32, one, dev), _plain(w, "seq_len", seq_len, i32, one, dev),
@@ -198,10 +218,12 @@ def harts_gen_attn_index(tree_node_ptr, node_parent, node_fork_off, node_len, no
                          grow=0) -> GenAttnIndex:
     """Work lists for the queries (q_node, q_pos) on a cached forest (harts_gen.h)."""
     w = "harts_gen_attn_index"
-    arrs = [np.ascontiguousarray(np.asarray(a), dtype=np.int32) for a in
-            (tree_node_ptr, node_parent, node_fork_off, node_len, node_page_ptr, node_page, q_node, q_pos)]
-    if any(a.ndim != 1 for a in arrs) or len(arrs[0]) < 1:
-        _bad(w, "arrays have one dimension")
+    _int32(w, page=page, Hq=Hq, Hkv=Hkv, grow=grow)
+    arrs = [_int32_array(w, *x) for x in (("tree_node_ptr", tree_node_ptr), ("node_parent", node_parent), ("node_fork_off", node_fork_off),
+                                          ("node_len", node_len), ("node_page_ptr", node_page_ptr), ("node_page", node_page), ("q_node", q_node),
+                                          ("q_pos", q_pos))]
+    if len(arrs[0]) < 1:
+        _bad(w, "tree_node_ptr is empty")
     n_nodes = int(arrs[0][-1])
     if [len(a) for a in arrs[1:5]] != [n_nodes] * 3 + [n_nodes + 1] or len(arrs[5]) != arrs[4][-1] or len(arrs[6]) != len(arrs[7]):
         _bad(w, "lengths of the arrays do not agree")

@@ -148,3 +148,26 @@ def test_pointers_that_do_not_ascend_are_refused_before_they_are_followed(bad):
     with pytest.raises(H.HartsError) as e:
         H.harts_gen_attn_index(**{**GOOD, **bad})
     assert e.value.code == -1
+
+
+W = 1 << 32
+
+
+@pytest.mark.parametrize("bad", [dict(q_pos=[4 + W]), dict(q_node=[1 - W]), dict(node_len=[10, 5 + W]), dict(node_page=[3, 4 + W]), dict(tree_node_ptr=[0, 2 + W]),
+                                 dict(node_parent=[-1, W]), dict(node_fork_off=[0, 10 + W]), dict(node_page_ptr=[0, 1, 2 - W]), dict(page=16 + W), dict(Hq=4 + W),
+                                 dict(Hkv=2 - W), dict(grow=W), dict(q_pos=np.array([4 + W], np.uint64)), dict(q_pos=np.array([2 ** 31], np.uint32)),
+                                 dict(q_pos=[4.5]), dict(q_pos=[[4]]), dict(q_pos=[float("nan")]), dict(node_page=[3.0, 1e20])])
+def test_numbers_that_32_bits_do_not_hold_are_refused(bad):
+    """They were cut off before: 2^32 + 4 was position 4."""
+    with pytest.raises(H.HartsError) as e:
+        H.harts_gen_attn_index(**{**GOOD, **bad})
+    assert e.value.code == -1
+
+
+@pytest.mark.parametrize("kind", [np.int8, np.int16, np.int32, np.int64, np.uint32, np.uint64, np.float32, np.float64])
+def test_whole_numbers_of_any_type_are_taken(kind):
+    want = H.harts_gen_attn_index(**GOOD).host
+    arrays = {k: np.asarray(v, kind) for k, v in GOOD.items() if isinstance(v, list) and min(v) >= 0}
+    assert np.array_equal(H.harts_gen_attn_index(**{**GOOD, **arrays}).host, want)
+    strided = {k: np.repeat(v, 2)[::2] for k, v in arrays.items()}
+    assert np.array_equal(H.harts_gen_attn_index(**{**GOOD, **strided}).host, want)

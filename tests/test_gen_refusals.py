@@ -148,3 +148,13 @@ def test_attn_refuses_a_scale_that_base_2_exponents_cannot_hold(scale, code):
     """scale / ln 2 in fp32; the one below it is taken (of a call without queries, which launches nothing)."""
     ix = index() if code else index(q_node=[], q_pos=[])
     assert gen.lib.harts_gen_attn(*{**dict(host=ix.host_ptr, dev=P), **ATTN, "scale": float(scale)}.values()) == code
+
+
+@pytest.mark.parametrize("at", [0, 1, 3, 4])
+def test_sizes_that_32_bits_do_not_hold_are_refused(at):
+    sizes = [3, 40, 120, 4, 128, 128]
+    assert H.harts_gen_la_workspace_bytes(*sizes, torch.bfloat16) > 0
+    sizes[at] += 1 << 32
+    with pytest.raises(H.HartsError) as e:
+        H.harts_gen_la_workspace_bytes(*sizes, torch.bfloat16)
+    assert e.value.code == EINVAL
