@@ -206,7 +206,7 @@ narrow_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q,
             for (int r = 0; r < NR; r++)
 #pragma unroll
                 for (int x = 0; x < 4; x++) s[r][x] = s2[r][x] = 0.f;
-            float kp[2] = {1.f, 1.f};
+            [[maybe_unused]] float kp[2] = {1.f, 1.f};
             if constexpr (F8) {
                 const unsigned char* se = smem + S::exps + 2 * rk.st * S::EXP + 16 * warp;
                 kp[0] = gen_power(se[g]);
