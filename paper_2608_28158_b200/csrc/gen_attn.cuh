@@ -97,13 +97,13 @@ struct PageWalk {
     }
 };
 
-// What brings a row of bf16 queries to 2^to: 2^x with x = to less the largest exponent (top: bits of the largest magnitude); zeros,
+// What brings a row of bf16 queries to 2^to: 2^x with x = to less the largest exponent (top: bits of the largest magnitude);
 // infinities and NaN as they are.  Applied in two steps, as 2^x may be beyond fp32's powers.
 struct PowerOfTwo {
     float f1, f2;
     int x1, x2;
     __device__ __forceinline__ PowerOfTwo(uint32_t top, int to) {
-        const int e = (int)(top >> 7), x = e == 0 || e == 255 ? 0 : to + 127 - e;
+        const int e = (int)(top >> 7), x = e == 255 ? 0 : to + 127 - max(e, 1);        // (subnormal rows: as the smallest normal ones)
         x1 = x / 2;
         x2 = x - x1;
         f1 = __uint_as_float((uint32_t)(127 + x1) << 23);

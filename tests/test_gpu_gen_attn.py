@@ -557,3 +557,12 @@ def test_keys_of_any_size_in_an_8_bit_cache(branches, q_scale, lo, hi):
     tree.values[0] = tree.cache[0].float().double() * (e.cpu().double() - 127).exp2().cuda()[..., None]
     index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 23, q_scale=q_scale)
     assert (index.n_wide > 0) == (branches > 16)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches", [2, 40])
+def test_subnormal_queries(kind, branches):
+    """Rows whose largest is below 2^-126, and a scale that makes scores of some units of them."""
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 27)
+    index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 27, q_scale=2.0 ** -129, scale=2.0 ** 126)
+    assert (index.n_wide > 0) == (branches > 16)
