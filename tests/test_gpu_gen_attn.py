@@ -566,3 +566,15 @@ def test_subnormal_queries(kind, branches):
     tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 27)
     index = check(tree, list(range(1, branches + 1)), [69] * branches, 4, 27, q_scale=2.0 ** -129, scale=2.0 ** 126)
     assert (index.n_wide > 0) == (branches > 16)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches,prefix", [(1, 500), (24, 2500)])
+def test_an_index_of_mostly_growth(kind, branches, prefix):
+    """Branches of a few tokens with room for thousands, at the first step, in between and at the last one."""
+    rng = random.Random(branches)
+    ln, grow = [prefix] + [rng.randint(0, 40) for _ in range(branches)], 3000
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [prefix] * branches, ln, 64, 2, kind, 28, grow=grow)
+    node, pos = list(range(1, branches + 1)), [n - 1 for n in ln[1:]]
+    for step in (0, 1, 777, grow):
+        check(tree, node, pos, 4, step, later=[p + step for p in pos])

@@ -328,3 +328,8 @@ def test_bases_of_16_bytes_alignment_only(lens, heads, pool_off, ws_off):
     H.harts_gen_la(q, k, v, g, o2, pool, dev(begin), dev(lens), dev(ins), dev(outs), max(lens), workspace=ws, dev_status=status)
     H.harts_la_check(status)
     assert torch.equal(o1, o2) and torch.equal(first, pool)
+
+
+@pytest.mark.parametrize("lens,heads", [([1] * 60 + [2000], 32), ([5000, 1, 1, 40, 1, 3000] + [1] * 30, 16), ([1, 1, 2500, 0, 13, 1], 48)])
+def test_single_tokens_and_prompts_in_one_call(lens, heads):
+    check(lens, heads, 128, "bf16", seed=14)
