@@ -361,8 +361,8 @@ wide_kernel(const Tables t, const __nv_bfloat16* __restrict__ q, int64_t ld_q, c
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
             }
-            const float top = mx * sc, by = m_ref == -INFINITY ? -INFINITY : -neg_m;
-            const bool raise = top > by + RAISE || (m_ref == -INFINITY && top > -INFINITY);
+            const float top = mx * sc;
+            const bool raise = top > RAISE - neg_m || (m_ref == -INFINITY && top > -INFINITY);
             if (__any_sync(~0u, raise)) {
                 const float m_new = raise ? F8 ? top : mx * scale_log2 : m_ref;
                 if (n > 0) {
