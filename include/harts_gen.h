@@ -51,7 +51,8 @@ extern "C" {
  * Served: fp32 with dk = dv = 64 or 128, bf16 with dk = dv = 64 or 128; chunks on the tensor cores for bf16 with 128, the others
  * walk token by token whatever their length.  States are fp32 and so are all sums; on the tensor cores the weighted keys are three bf16 terms each, so
  * that states keep fp32's accuracy, while scores and the states that outputs are made of are rounded to bf16, as in harts_la.h.
- * There, an infinity or a NaN in a row's k or v can also reach the outputs (not the states) of the rows ahead of it in its chunk.
+ * There, an infinity or a NaN in a row's k or v can also reach the outputs (not the states) of the rows ahead of it in its chunk, and an infinity
+ * in k makes NaN of what it makes infinite token by token.
  * A sequence with a bad entry is left out (dev_status[1] = its number).
  * Errors: HARTS_EINVAL (null or misaligned pointer, size out of range, workspace too small), HARTS_EUNSUPPORTED, HARTS_ECUDA.
  */
@@ -104,13 +105,15 @@ int32_t harts_gen_cache_read(int64_t n, const int32_t* slot, const void* k_cache
  *   Tokens that several queries see are read once for up to 128 rows (a row: a query and a head of its group), long runs are split over the GPU.
  *   grow: by how many tokens nodes with queries may grow while the index is used: between calls (and replays of a captured call) q_pos may
  *   go up, to node_len - 1 + grow at most and as far as the node's listed pages go, and never below what it was for the index.
- *   A new branch, a fork, or a query more or less needs a new index.
+ *   A new branch, a fork, or a query more or less needs a new index.  Work is divided as if all that room were tokens, so ask for what will be
+ *   used: 64 branches of 1,200 on 16,421 tokens take 64 us with no room, 66 with 256 tokens of it, 88 with 1,024, 100 with 4,096.
  *   cap_words: capacity of blob, which may be NULL to get *n_words only.
  *   Errors: HARTS_EINVAL (malformed forest, pages missing or negative, q_pos out of range, capacity), HARTS_ENOMEM.
  * harts_gen_attn_workspace_bytes: of the parts of split sums.  Calls that share a workspace must not run at the same time.
  * harts_gen_attn: q bf16 [n_q, Hq, 128], heads contiguous, ld_q elements between rows; q_pos device int32 [n_q]; o bf16, lse fp32,
  *   contiguous, written for every query, neither overlapping an input.  An out-of-range q_pos is brought into its range and reported (dev_status[1] = the query).
- *   scale is positive and at most FLT_MAX ln 2 (2.3e38).  Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded to bf16 for the second product.
+ *   scale is positive and at most FLT_MAX ln 2 (2.3e38).  Products on the tensor cores with fp32 sums; softmax in fp32, its values rounded for the
+ *   second product: to bf16, or, of an 8-bit cache, to fp16 in the kernel for up to 16 rows.
  */
 #define HARTS_GEN_ATTN_HEADER_WORDS 32
 int32_t harts_gen_attn_index(int32_t n_trees, const int32_t* tree_node_ptr, const int32_t* node_parent, const int32_t* node_fork_off,

@@ -3,7 +3,8 @@
 // Eight lanes a row of 128: each has 16 values, so that a row is read by eight 32-byte pieces and written as 8-bit values by eight
 // 16-byte ones.  The scale being a power of two, x 2^-e is exact and rounding is that of the significand alone (values far below the
 // row's largest lose bits as subnormals do).  Bound by the traffic, 512 + 258 bytes a (token, head)
-// either way: 16,385 tokens x 8 heads written in 19.2 us (5.3 TB/s), 24,000 x 4 read in 13.3 (5.6), launches of 4 to 5 us apart.
+// either way: 16,385 tokens x 8 heads written in 21.3 us (4.7 TB/s), 24,000 x 4 read in 16.1 (4.6); kernels alone, inputs larger than the L2.
+// bf16, call and launch: 16,385 x 8 in 25.0 either way (0.82 of a copy), 24,000 x 4 in 20.5 (0.74).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 

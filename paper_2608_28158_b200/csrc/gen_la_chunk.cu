@@ -1,7 +1,7 @@
 // Linear attention from and into kept states in chunks (bf16, d = 128): the work table, and what lets several CTAs share one long
 // sequence.
 //
-// The walk itself is pipe_fwd_kernel (la_pipe_fwd.cu): 2.2 us a chunk and head where the chain of chunks is what counts.  A sequence that
+// The walk itself is pipe_fwd_kernel (la_pipe_fwd.cu): 2.2 us a chunk and head where a chain of chunks is all that an SM has, 3 in a mix.  A sequence that
 // is long beside what every SM has to do is cut into segments of L chunks, whose start states are found first:
 //     U_i = sum over segment i of e^{B_end - B_j} k_j^T v_j,   S_{i+1} = e^{B_i} S_i + U_i
 // The sums do not depend on each other (one product of k~^T v with the tokens as its inner dimension, left in tensor memory until the

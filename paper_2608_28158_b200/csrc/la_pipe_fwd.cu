@@ -21,7 +21,7 @@
 // the given keys and values, so a weighted key is three bf16 terms (two leave 2.3e-6 of a state, three 1.5 to 4.5e-7), two of them in tiles of their
 // own, and K~^T V three products.  The room is that of the second tile of P, and masking has a barrier of its own, off the chain of sums.
 // Rows behind an item's end belong to others and may hold anything: a partial chunk's keys and values are zeroed there.
-// 2.2 us a chunk: 1.3 of weighing, then 0.6 of the products, one after the other on the one pair of tiles for the further terms.  Weighing is
+// 2.2 us a chunk (148 items of 16 to 48 chunks, an SM each; beside others' switches 3, which is what the planning kernel reckons with): 1.3 of weighing, then 0.6 of the products, one after the other on the one pair of tiles for the further terms.  Weighing is
 // one function out of line for all warps that do it, since its copies did not fit the instruction cache beside the rest (31,017 tokens x 4
 // heads in 35 segments, whole call then: 89 -> 80 us).
 //
