@@ -578,3 +578,31 @@ def test_an_index_of_mostly_growth(kind, branches, prefix):
     node, pos = list(range(1, branches + 1)), [n - 1 for n in ln[1:]]
     for step in (0, 1, 777, grow):
         check(tree, node, pos, 4, step, later=[p + step for p in pos])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("branches", [2, 40])
+def test_tensors_of_16_bytes_alignment_only(kind, branches):
+    """Cache, powers, queries, outputs, index and workspace 16 bytes past a multiple of 256: written, read and attended to as elsewhere."""
+    def at_16(x):
+        n = x.numel() * x.element_size()
+        buf = torch.full((n + 512,), 255, dtype=torch.uint8, device="cuda")
+        off = -buf.data_ptr() % 256 + 16
+        return buf[off:off + n].view(x.dtype).view(x.shape).copy_(x)
+
+    tree = Tree([0, branches + 1], [-1] + [0] * branches, [0] + [700] * branches, [700] + [70] * branches, 32, 2, kind, 29)
+    node, pos = list(range(1, branches + 1)), [69] * branches
+    index, q = tree.index(node, pos, 4), queries(branches, 8, 29)
+    rows = [torch.randn(700, 2, 128, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    slot = tree.slots[0].int()
+    got = []
+    for place in (torch.clone, at_16):
+        cache, exps = [place(x) for x in tree.cache], [None if x is None else place(x) for x in tree.exp]
+        H.harts_gen_cache_write(*(place(x) for x in rows), place(slot), *cache, *exps)
+        back = [place(x) for x in rows]
+        H.harts_gen_cache_read(*cache, place(slot), *back, *exps)
+        index.dev = place(index.dev)
+        o, lse, ws = place(q), place(torch.empty(q.shape[:2], device="cuda")), place(torch.zeros(max(16, index.workspace_bytes), dtype=torch.uint8, device="cuda"))
+        H.harts_gen_attn(index, place(q), *cache, place(torch.tensor(pos, dtype=torch.int32, device="cuda")), o, lse, 0.1, ws, *exps)
+        got.append(back + [o, lse])
+    assert all(torch.equal(a, b) for a, b in zip(*got))

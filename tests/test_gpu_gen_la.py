@@ -333,3 +333,24 @@ def test_bases_of_16_bytes_alignment_only(lens, heads, pool_off, ws_off):
 @pytest.mark.parametrize("lens,heads", [([1] * 60 + [2000], 32), ([5000, 1, 1, 40, 1, 3000] + [1] * 30, 16), ([1, 1, 2500, 0, 13, 1], 48)])
 def test_single_tokens_and_prompts_in_one_call(lens, heads):
     check(lens, heads, 128, "bf16", seed=14)
+
+
+def at_16(x):
+    """x in a buffer of its own, 16 bytes past a multiple of 256."""
+    n = x.numel() * x.element_size()
+    buf = torch.full((n + 512,), 255, dtype=torch.uint8, device="cuda")
+    off = -buf.data_ptr() % 256 + 16
+    y = buf[off:off + n].view(x.dtype).view(x.shape)
+    return y.copy_(x)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 64), ("fp32", 128)])
+@pytest.mark.parametrize("lens", [[1, 3, 1], [30, 0, 130, 700]])
+def test_tensors_of_16_bytes_alignment_only(dtype, d, lens):
+    q, k, v, g, states, begin, ins, outs = problem(lens, 3, d, dtype, 15, gaps=1)
+    pool = at_16(states)
+    o1, _ = call(q, k, v, g, states, begin, lens, ins, outs)
+    o2 = at_16(torch.full_like(v, float("nan")))
+    _, status = call(at_16(q), at_16(k), at_16(v), at_16(g), pool, begin, lens, ins, outs, o=o2)
+    H.harts_la_check(status)
+    assert torch.equal(torch.nan_to_num(o1), torch.nan_to_num(o2)) and torch.equal(torch.isnan(o1), torch.isnan(o2)) and torch.equal(states, pool)
